@@ -44,7 +44,7 @@
 extern "C" {
 #endif
 
-#define ATTN_ABI_VERSION 4
+#define ATTN_ABI_VERSION 5
 
 /* Largest attn_variant_desc.num_segments, and num_global when global_tokens
  * lists the global positions (both are staged on chip). */
@@ -258,6 +258,175 @@ int attn_fwd(const void *q, const void *k, const void *v, void *out, float *lse,
 int64_t attn_workspace_bytes(const attn_variant_desc *desc);
 int attn_fwd_ws(const void *q, const void *k, const void *v, void *out, float *lse,
                 const attn_variant_desc *desc, void *workspace, int64_t workspace_bytes);
+
+/* ---- 8-bit block cache ------------------------------------------------------
+ *
+ * Keys and values of a serving batch, in a pool of blocks of block_size tokens,
+ * in 8-bit floating point with one fp32 scale for each block and kv head (and
+ * one for K, one for V): a stored value x stands for x * scale. A request's
+ * tokens lie in the blocks its row of the block table lists, position p in
+ * block_tables[request][p / block_size] at place p % block_size.
+ *
+ * A step of a server: attn_cache_plan gives the new tokens blocks and slots
+ * (slot = block * block_size + place), attn_cache_append writes their keys and
+ * values, attn_cache_fwd attends to the cache. All three only enqueue work on
+ * the caller's stream, read lengths and tables on the device, and can be
+ * captured into a graph.
+ */
+typedef enum attn_cache_dtype {
+    ATTN_E4M3 = 0, /* 4 exponent and 3 mantissa bits, largest value 448, no infinities */
+    ATTN_E5M2 = 1  /* 5 exponent and 2 mantissa bits, largest value 57344              */
+} attn_cache_dtype_t;
+
+/*
+ * The pool. K of a block is [block_size][head_dim], V is the transpose,
+ * [head_dim][block_size] (a wavefront then reads both in the operand order of
+ * its matrix products), each contiguous:
+ *   k [num_blocks, num_kv_heads, block_size, head_dim]  k_scale [num_blocks, num_kv_heads]
+ *   v [num_blocks, num_kv_heads, head_dim, block_size]  v_scale [num_blocks, num_kv_heads]
+ * Strides are in elements; 0 selects the contiguous default. A block of one
+ * head must not overlap another's. Scales are finite and >= 0; those of blocks
+ * that no token uses, like the bytes behind a request's last token, may hold
+ * anything.
+ */
+typedef struct attn_cache {
+    uint32_t struct_size;   /* sizeof(attn_cache)                                  */
+    int32_t cache_dtype;    /* attn_cache_dtype_t                                  */
+    int32_t num_blocks;     /* > 0                                                 */
+    int32_t num_kv_heads;   /* > 0                                                 */
+    int32_t block_size;     /* 16, 32, 64 or 128                                   */
+    int32_t head_dim;       /* 64 or 128                                           */
+    void *k, *v;            /* device, 16-byte aligned                             */
+    float *k_scale, *v_scale;
+    int64_t stride_k_block, stride_k_head;   /* multiples of 16                    */
+    int64_t stride_v_block, stride_v_head;
+    int64_t stride_ks_block, stride_vs_block; /* heads of a block are contiguous   */
+} attn_cache;
+
+/*
+ * attn_cache_plan: blocks and slots of a step's new tokens from the requests'
+ * lengths, in one kernel. Request r holds cached_lens[r] tokens and gets
+ * new_lens[r] more (both >= 0, the sum below 2^31). It needs
+ *   need_r = ceil((cached + new) / block_size) - ceil(cached / block_size)
+ * blocks. The requests take theirs in order from the end of the list of free
+ * blocks: with off_r = sum of need over the requests before r, the u-th new
+ * block of request r is free_blocks[n - 1 - off_r - u], n = *num_free. A request
+ * is refused, keeps its cached tokens and takes no block when off_r + need_r > n
+ * and need_r > 0, or when its blocks do not fit its row of the table (it then
+ * counts with need 0). Outputs:
+ *   block_tables  entries of the new blocks, in place (others are left alone)
+ *   slots         [total_new], the new tokens of request r at cu_seqlens_q[r] on
+ *                 in order of position; -1 for those of a refused request, for
+ *                 those in a block whose table entry is negative, and past the
+ *                 last request's
+ *   cu_seqlens_q  [batch + 1] prefix sums of new_lens (of refused requests too)
+ *   seqlens_k     [batch] cached + new, or cached where refused
+ *   num_free_out  [1] n less the blocks taken (may not be num_free itself)
+ * total_new >= the sum of new_lens; tokens past it get no slot. A num_free
+ * outside [0, free_len] is taken as the nearer end.
+ */
+typedef struct attn_cache_plan_desc {
+    uint32_t struct_size;
+    int32_t batch;               /* >= 0                                           */
+    int32_t block_size;          /* 16, 32, 64 or 128                              */
+    int32_t table_width;         /* columns of block_tables, >= 0                  */
+    int64_t stride_table;        /* elements between its rows; 0 = table_width     */
+    int32_t free_len;            /* entries of free_blocks, >= 0                   */
+    uint32_t flags;              /* ATTN_FLAG_LOG                                  */
+    int64_t total_new;           /* 0 .. 2^31 - 1                                  */
+    const int32_t *cached_lens;  /* device [batch]                                 */
+    const int32_t *new_lens;     /* device [batch]                                 */
+    int32_t *block_tables;       /* device [batch, table_width]                    */
+    const int32_t *free_blocks;  /* device [free_len]                              */
+    const int32_t *num_free;     /* device [1]                                     */
+    int64_t *slots;              /* device [total_new]                             */
+    int32_t *cu_seqlens_q;       /* device [batch + 1]                             */
+    int32_t *seqlens_k;          /* device [batch]                                 */
+    int32_t *num_free_out;       /* device [1]                                     */
+    void *stream;
+} attn_cache_plan_desc;
+
+int attn_cache_plan(const attn_cache_plan_desc *desc);
+
+/*
+ * attn_cache_append: write new keys and values into the cache. k, v are
+ * [total_new, num_kv_heads, head_dim] (bf16 or fp32) with the strides of the
+ * descriptor; token t goes to slots[t]. For each block and head that gets tokens
+ *   a = largest finite |x| of its new values, e = the smallest integer >= -120
+ *       with a <= MAX 2^e,
+ *   scale' = max(2^e, its scale before) if the block holds earlier tokens (the
+ *       first new one is not at place 0), else 2^e;
+ * new values are stored as x / scale', earlier ones, where the scale grew, as
+ * q * scale / scale' from their stored q, each rounded to nearest even and
+ * limited to +-MAX (448 or 57344; infinities become +-MAX 2^e, NaN stays NaN).
+ * Powers of two make both steps exact but for the rounding of values that
+ * become subnormal: growth does not round twice.
+ * The tokens of one block stand together in `slots`, at places ascending by
+ * one (what attn_cache_plan gives), and a block is named by one run of tokens
+ * only: two runs of one block race for its scale. ATTN_FLAG_VALIDATE checks
+ * that (ATTN_ERR_BAD_SHAPE). A slot outside the pool is skipped.
+ */
+typedef struct attn_cache_append_desc {
+    uint32_t struct_size;
+    int32_t dtype;               /* attn_dtype_t of k and v                        */
+    int64_t total_new;           /* 0 .. 2^31 - 1                                  */
+    int64_t stride_k_h, stride_k_s, stride_v_h, stride_v_s; /* multiples of 16 bytes */
+    const int64_t *slots;        /* device [total_new]                             */
+    void *stream;
+    uint32_t flags;              /* ATTN_FLAG_*                                    */
+} attn_cache_append_desc;
+
+int attn_cache_append(const void *k, const void *v, const attn_cache *cache,
+                      const attn_cache_append_desc *desc);
+
+/*
+ * attn_cache_fwd: softmax attention of new queries to the cached keys of their
+ * requests. Layouts of q, out and lse, the score (scale, soft-cap, ALiBi), the
+ * bottom-right alignment and the rows without a visible key are those of
+ * attn_fwd; the masks are NONE, CAUSAL and SLIDING_WINDOW. Request r has
+ * seqlens_k[r] keys, its own new ones included (attn_cache_append runs first).
+ *   cu_seqlens_q == NULL: seqlen_q queries of every request, q [batch, num_q_heads,
+ *   seqlen_q, head_dim]; otherwise packed q [total_q, num_q_heads, head_dim].
+ * Keys of a table entry outside the pool, and past the table's width, are not
+ * visible; a key that no row of a workgroup's tile of rows sees leaves them
+ * alone whatever its bytes, an infinite or NaN V of one that some row sees may
+ * reach others of the same request. Packed rows behind the last request's keep
+ * their output. Arithmetic: products of the stored values with q in bf16 matrix
+ * instructions and fp32 sums, the scales applied in fp32 (fp32 q and P are split
+ * into three bf16 terms, so nothing is lost).
+ * The workspace is that of attn_fwd_ws: attn_cache_workspace_bytes says how much
+ * the call can use, NULL or less computes it without splitting the keys.
+ */
+typedef struct attn_cache_fwd_desc {
+    uint32_t struct_size;
+    int32_t dtype;               /* attn_dtype_t of q and out                      */
+    int32_t batch;               /* >= 0                                           */
+    int32_t num_q_heads;         /* a multiple of the cache's num_kv_heads         */
+    int32_t seqlen_q;            /* fixed length only                              */
+    int32_t max_seqlen_q;        /* packed: >= every query length                  */
+    int64_t total_q;             /* packed: rows of q                              */
+    int32_t max_seqlen_k;        /* about the longest key length (sizes the key
+                                    splits; a longer request is computed all the
+                                    same); 0: table_width * block_size             */
+    int32_t table_width;
+    int64_t stride_table;        /* elements; 0 = table_width                      */
+    const int32_t *block_tables; /* device [batch, table_width]                    */
+    const int32_t *seqlens_k;    /* device [batch]                                 */
+    const int32_t *cu_seqlens_q; /* device [batch + 1], or NULL (fixed length)     */
+    const float *alibi_slopes;   /* device [num_q_heads] or NULL                   */
+    float scale, softcap;
+    int32_t mask_kind, window_left, window_right;
+    uint32_t flags;              /* ATTN_FLAG_*; VALIDATE checks cu_seqlens_q,
+                                    seqlens_k (BAD_SHAPE) and the table entries in
+                                    use (BAD_VARIANT)                              */
+    int64_t stride_q_b, stride_q_h, stride_q_s;
+    int64_t stride_o_b, stride_o_h, stride_o_s;
+    void *stream;
+} attn_cache_fwd_desc;
+
+int64_t attn_cache_workspace_bytes(const attn_cache *cache, const attn_cache_fwd_desc *desc);
+int attn_cache_fwd(const void *q, void *out, float *lse, const attn_cache *cache,
+                   const attn_cache_fwd_desc *desc, void *workspace, int64_t workspace_bytes);
 
 /* Static description of an error code (never NULL). */
 const char *attn_status_string(int status);

@@ -24,12 +24,15 @@ from ._abi import (ATTN_BF16, ATTN_FLAG_LOG, ATTN_FLAG_VALIDATE, ATTN_FP32, ATTN
                    ATTN_MASK_PREFIX_LM, ATTN_MASK_SHARE_QUESTION, ATTN_MASK_SLIDING_WINDOW,
                    ATTN_MAX_SEGMENTS, ATTN_NORM_RELU, ATTN_NORM_SIGMOID, ATTN_NORM_SOFTMAX,
                    AttnError, AttnVariantDesc, check, load, plan_tiles, row_range)
+from .cache import (CachePlan, KVCache, cache_append, cache_fwd, cache_plan,  # noqa: F401
+                    new_cache)
 
 __all__ = ["fwd", "make_desc", "lse_shape", "AttnError", "AttnVariantDesc", "load", "plan_tiles",
            "row_range", "ATTN_BF16", "ATTN_FP32", "ATTN_MASK_NONE", "ATTN_MASK_CAUSAL",
            "ATTN_MASK_SLIDING_WINDOW", "ATTN_MASK_PREFIX_LM", "ATTN_MASK_GLOBAL_SLIDING_WINDOW",
            "ATTN_MASK_SHARE_QUESTION", "ATTN_MASK_CAUSAL_BLOCKWISE", "ATTN_NORM_SOFTMAX",
-           "ATTN_NORM_RELU", "ATTN_NORM_SIGMOID", "ATTN_FLAG_VALIDATE", "ATTN_FLAG_LOG"]
+           "ATTN_NORM_RELU", "ATTN_NORM_SIGMOID", "ATTN_FLAG_VALIDATE", "ATTN_FLAG_LOG",
+           "KVCache", "CachePlan", "new_cache", "cache_plan", "cache_append", "cache_fwd"]
 
 _DTYPES = {torch.bfloat16: ATTN_BF16, torch.float32: ATTN_FP32}
 _MASKS = {"none": ATTN_MASK_NONE, "causal": ATTN_MASK_CAUSAL,

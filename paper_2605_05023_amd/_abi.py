@@ -12,7 +12,7 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libattn.so")
 
-ATTN_ABI_VERSION = 4
+ATTN_ABI_VERSION = 5
 ATTN_MAX_SEGMENTS = 2048
 ATTN_FLAG_VALIDATE = 1
 ATTN_FLAG_LOG = 2
@@ -21,6 +21,7 @@ ATTN_MASK_NONE, ATTN_MASK_CAUSAL, ATTN_MASK_SLIDING_WINDOW = 0, 1, 2
 ATTN_MASK_PREFIX_LM, ATTN_MASK_GLOBAL_SLIDING_WINDOW = 3, 4
 ATTN_MASK_SHARE_QUESTION, ATTN_MASK_CAUSAL_BLOCKWISE = 5, 6
 ATTN_NORM_SOFTMAX, ATTN_NORM_RELU, ATTN_NORM_SIGMOID = 0, 1, 2
+ATTN_E4M3, ATTN_E5M2 = 0, 1
 
 STATUS = {
     0: "ATTN_OK",
@@ -35,10 +36,93 @@ STATUS = {
 STATUS_CODE = {v: k for k, v in STATUS.items()}
 
 EXPORTED = ("attn_fwd", "attn_fwd_ws", "attn_workspace_bytes", "attn_status_string", "attn_abi_version",
-            "attn_plan_tiles", "attn_row_range")
+            "attn_plan_tiles", "attn_row_range", "attn_cache_plan", "attn_cache_append", "attn_cache_fwd",
+            "attn_cache_workspace_bytes")
 
 
-class AttnVariantDesc(ctypes.Structure):
+class _Sized(ctypes.Structure):
+    """A descriptor that begins with its own size."""
+
+    @classmethod
+    def new(cls):
+        d = cls()
+        d.struct_size = ctypes.sizeof(cls)
+        return d
+
+
+class AttnCache(_Sized):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("cache_dtype", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("block_size", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("stride_k_block", ctypes.c_int64), ("stride_k_head", ctypes.c_int64),
+        ("stride_v_block", ctypes.c_int64), ("stride_v_head", ctypes.c_int64),
+        ("stride_ks_block", ctypes.c_int64), ("stride_vs_block", ctypes.c_int64),
+    ]
+
+
+class AttnCachePlanDesc(_Sized):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("batch", ctypes.c_int32),
+        ("block_size", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("stride_table", ctypes.c_int64),
+        ("free_len", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("total_new", ctypes.c_int64),
+        ("cached_lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+        ("block_tables", ctypes.c_void_p), ("free_blocks", ctypes.c_void_p),
+        ("num_free", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+        ("cu_seqlens_q", ctypes.c_void_p), ("seqlens_k", ctypes.c_void_p),
+        ("num_free_out", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class AttnCacheAppendDesc(_Sized):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32),
+        ("total_new", ctypes.c_int64),
+        ("stride_k_h", ctypes.c_int64), ("stride_k_s", ctypes.c_int64),
+        ("stride_v_h", ctypes.c_int64), ("stride_v_s", ctypes.c_int64),
+        ("slots", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+        ("flags", ctypes.c_uint32),
+    ]
+
+
+class AttnCacheFwdDesc(_Sized):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("seqlen_q", ctypes.c_int32),
+        ("max_seqlen_q", ctypes.c_int32),
+        ("total_q", ctypes.c_int64),
+        ("max_seqlen_k", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("stride_table", ctypes.c_int64),
+        ("block_tables", ctypes.c_void_p), ("seqlens_k", ctypes.c_void_p),
+        ("cu_seqlens_q", ctypes.c_void_p), ("alibi_slopes", ctypes.c_void_p),
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+        ("mask_kind", ctypes.c_int32),
+        ("window_left", ctypes.c_int32), ("window_right", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("stride_q_b", ctypes.c_int64), ("stride_q_h", ctypes.c_int64), ("stride_q_s", ctypes.c_int64),
+        ("stride_o_b", ctypes.c_int64), ("stride_o_h", ctypes.c_int64), ("stride_o_s", ctypes.c_int64),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+class AttnVariantDesc(_Sized):
     _fields_ = [
         ("struct_size", ctypes.c_uint32),
         ("dtype", ctypes.c_int32),
@@ -81,12 +165,6 @@ class AttnVariantDesc(ctypes.Structure):
         ("global_stride", ctypes.c_int64),
     ]
 
-    @classmethod
-    def new(cls) -> "AttnVariantDesc":
-        d = cls()
-        d.struct_size = ctypes.sizeof(cls)
-        return d
-
 
 class AttnError(RuntimeError):
     def __init__(self, status: int, msg: str):
@@ -125,6 +203,17 @@ def load(path: str = LIB_PATH):
     lib.attn_row_range.argtypes = [ctypes.POINTER(AttnVariantDesc), ctypes.POINTER(ctypes.c_int32),
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.POINTER(ctypes.c_int32)]
+    lib.attn_cache_plan.restype = ctypes.c_int
+    lib.attn_cache_plan.argtypes = [ctypes.POINTER(AttnCachePlanDesc)]
+    lib.attn_cache_append.restype = ctypes.c_int
+    lib.attn_cache_append.argtypes = [ctypes.c_void_p] * 2 + [ctypes.POINTER(AttnCache),
+                                                              ctypes.POINTER(AttnCacheAppendDesc)]
+    lib.attn_cache_workspace_bytes.restype = ctypes.c_int64
+    lib.attn_cache_workspace_bytes.argtypes = [ctypes.POINTER(AttnCache),
+                                               ctypes.POINTER(AttnCacheFwdDesc)]
+    lib.attn_cache_fwd.restype = ctypes.c_int
+    lib.attn_cache_fwd.argtypes = [ctypes.c_void_p] * 3 + [
+        ctypes.POINTER(AttnCache), ctypes.POINTER(AttnCacheFwdDesc), ctypes.c_void_p, ctypes.c_int64]
     if lib.attn_abi_version() != ATTN_ABI_VERSION:
         raise ImportError("libattn.so ABI version mismatch")
     if path == LIB_PATH:

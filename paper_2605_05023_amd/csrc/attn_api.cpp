@@ -13,10 +13,15 @@
 #include <vector>
 
 #include "../../include/attn.h"
+#include "api_util.h"
 #include "kernel_params.h"
 #include "launch.h"
 #include "row_vis.h"
 #include "softcap_poly.h"
+
+using attn::aligned16;
+using attn::fetch;
+using attn::rows_disjoint;
 
 namespace {
 
@@ -25,8 +30,6 @@ constexpr int64_t kMaxSplits = 64;
 // Flat query rows (query heads of a kv group x queries) that the decode kernel
 // may take: up to 64, and up to 128 while there are at most 256 kv groups.
 constexpr int64_t kDecodeFlatRows = 64, kDecodeFlatRowsFew = 128, kDecodeFewGroups = 256;
-
-bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
 
 // Resolve one tensor's strides (0 = contiguous default) and check them.
 // Returns ATTN_OK or an error code.
@@ -63,45 +66,6 @@ bool slice_fits(int64_t rows, int64_t stride_s, int64_t d, int64_t elt_bytes, in
     return bytes < (int64_t(1) << 31);
 }
 
-// Do the D-element rows of an output with these sizes and strides stay
-// disjoint? Ordered by stride, every dimension must step past the whole extent
-// of the ones inside it (sufficient, and what every ordinary layout meets);
-// dimensions of size one are ignored. Overlapping output rows would make the
-// result depend on which workgroup writes last.
-bool rows_disjoint(int64_t d, int n, const int64_t* size, const int64_t* stride)
-{
-    int64_t sz[3], st[3];
-    int m = 0;
-    for (int i = 0; i < n; ++i)
-        if (size[i] > 1) {
-            sz[m] = size[i];
-            st[m] = stride[i];
-            ++m;
-        }
-    for (int a = 0; a < m; ++a)  // insertion sort by stride
-        for (int b = a; b > 0 && st[b] < st[b - 1]; --b) {
-            int64_t t = st[b]; st[b] = st[b - 1]; st[b - 1] = t;
-            t = sz[b]; sz[b] = sz[b - 1]; sz[b - 1] = t;
-        }
-    int64_t extent = d;  // elements covered by one row
-    for (int a = 0; a < m; ++a) {
-        if (st[a] < extent) return false;
-        extent = st[a] * (sz[a] - 1) + extent;
-    }
-    return true;
-}
-
-// Host copy of a device int32 array, on `stream` (ATTN_FLAG_VALIDATE only).
-bool fetch_i32(const int32_t* dev, int64_t n, hipStream_t stream, std::vector<int32_t>* out)
-{
-    out->assign((size_t)n, 0);
-    if (n == 0) return true;
-    if (hipMemcpyAsync(out->data(), dev, (size_t)n * sizeof(int32_t), hipMemcpyDeviceToHost,
-                       stream) != hipSuccess)
-        return false;
-    return hipStreamSynchronize(stream) == hipSuccess;
-}
-
 bool strictly_increasing_nonneg(const std::vector<int32_t>& a)
 {
     for (size_t i = 0; i < a.size(); ++i)
@@ -119,7 +83,7 @@ int validate_device_inputs(const attn_variant_desc& d, bool varlen, bool segment
         const int64_t total[2] = {d.total_q, d.total_k};
         const int64_t maxlen[2] = {d.max_seqlen_q, d.max_seqlen_k};
         for (int t = 0; t < 2; ++t) {
-            if (!fetch_i32(cus[t], (int64_t)d.batch + 1, stream, &a)) return ATTN_ERR_LAUNCH;
+            if (!fetch(cus[t], (int64_t)d.batch + 1, stream, &a)) return ATTN_ERR_LAUNCH;
             if (a[0] != 0 || a[(size_t)d.batch] != total[t]) return ATTN_ERR_BAD_SHAPE;
             for (int32_t s = 0; s < d.batch; ++s) {
                 const int64_t len = (int64_t)a[(size_t)s + 1] - a[(size_t)s];
@@ -131,7 +95,7 @@ int validate_device_inputs(const attn_variant_desc& d, bool varlen, bool segment
     auto check_arrays = [&](const int32_t* base, int64_t n, int64_t stride) {
         const int64_t copies = stride > 0 ? d.batch : 1;
         for (int64_t s = 0; s < copies; ++s) {
-            if (!fetch_i32(base + s * stride, n, stream, &a)) return ATTN_ERR_LAUNCH;
+            if (!fetch(base + s * stride, n, stream, &a)) return ATTN_ERR_LAUNCH;
             if (!strictly_increasing_nonneg(a)) return ATTN_ERR_BAD_VARIANT;
         }
         return ATTN_OK;

@@ -1,0 +1,432 @@
+// cache_api.cpp -- C ABI of the 8-bit block cache: validation, planning and
+// dispatch of attn_cache_plan, attn_cache_append and attn_cache_fwd. As in
+// attn_api.cpp every check runs on the host before the first HIP call, and only
+// ATTN_FLAG_VALIDATE reads device memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+#include <unordered_set>
+#include <vector>
+
+#include "../../include/attn.h"
+#include "api_util.h"
+#include "cache_params.h"
+
+using attn::aligned16;
+using attn::CacheAppendParams;
+using attn::CacheFwdKind;
+using attn::CacheFwdParams;
+using attn::CachePlanParams;
+using attn::CachePool;
+using attn::fetch;
+using attn::rows_disjoint;
+
+namespace {
+
+constexpr int64_t kInt32Max = INT32_MAX;
+// The most key splits of a row tile (the combine kernel takes one per lane).
+constexpr int64_t kMaxSplits = 64;
+constexpr int64_t kChunkKeys = 64;  // keys a wavefront takes at a time
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// log2 of a supported block size, else -1.
+int block_shift(int32_t size)
+{
+    return size == 16 ? 4 : size == 32 ? 5 : size == 64 ? 6 : size == 128 ? 7 : -1;
+}
+
+bool bad_flags(uint32_t flags) { return (flags & ~(ATTN_FLAG_VALIDATE | ATTN_FLAG_LOG)) != 0; }
+
+// Check the pool but for its pointers, and resolve its strides.
+int check_cache(const attn_cache* c, CachePool* p)
+{
+    if (!c) return ATTN_ERR_NULL_PTR;
+    if (c->struct_size != sizeof(attn_cache)) return ATTN_ERR_ABI;
+    if (c->cache_dtype != ATTN_E4M3 && c->cache_dtype != ATTN_E5M2) return ATTN_ERR_UNSUPPORTED;
+    if (c->head_dim != 64 && c->head_dim != 128) return ATTN_ERR_UNSUPPORTED;
+    p->bshift = block_shift(c->block_size);
+    if (p->bshift < 0) return ATTN_ERR_UNSUPPORTED;
+    if (c->num_blocks <= 0 || c->num_kv_heads <= 0) return ATTN_ERR_BAD_SHAPE;
+    if (c->num_kv_heads > 65535) return ATTN_ERR_UNSUPPORTED;  // a grid axis
+    const int64_t page = (int64_t)c->block_size * c->head_dim, h = c->num_kv_heads;
+    const int64_t in[4] = {c->stride_k_block, c->stride_k_head, c->stride_v_block, c->stride_v_head};
+    int64_t out[4];
+    for (int i = 0; i < 4; ++i) {
+        if (in[i] < 0) return ATTN_ERR_BAD_SHAPE;
+        if (in[i] % 16) return ATTN_ERR_ALIGNMENT;
+        out[i] = in[i] ? in[i] : i % 2 ? page : h * page;
+    }
+    for (int i = 0; i < 4; i += 2) {
+        const int64_t size[2] = {c->num_blocks, h}, stride[2] = {out[i], out[i + 1]};
+        if (!rows_disjoint(page, 2, size, stride)) return ATTN_ERR_BAD_SHAPE;
+    }
+    p->sks_b = c->stride_ks_block ? c->stride_ks_block : h;
+    p->svs_b = c->stride_vs_block ? c->stride_vs_block : h;
+    if (c->num_blocks > 1 && (p->sks_b < h || p->svs_b < h)) return ATTN_ERR_BAD_SHAPE;
+    p->sk_b = out[0], p->sk_h = out[1], p->sv_b = out[2], p->sv_h = out[3];
+    p->num_blocks = c->num_blocks;
+    p->hkv = c->num_kv_heads;
+    return ATTN_OK;
+}
+
+int check_cache_pointers(const attn_cache* c, CachePool* p)
+{
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return ATTN_ERR_NULL_PTR;
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))
+        return ATTN_ERR_ALIGNMENT;
+    p->k = static_cast<uint8_t*>(c->k);
+    p->v = static_cast<uint8_t*>(c->v);
+    p->k_scale = c->k_scale;
+    p->v_scale = c->v_scale;
+    return ATTN_OK;
+}
+
+int launched(hipError_t err, uint32_t flags, const char* what)
+{
+    if (err != hipSuccess && (flags & ATTN_FLAG_LOG))
+        std::fprintf(stderr, "%s: launch failed: %s\n", what, hipGetErrorString(err));
+    return err == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+const char* format_name(const attn_cache* c) { return c->cache_dtype == ATTN_E4M3 ? "e4m3" : "e5m2"; }
+
+}  // namespace
+
+extern "C" int attn_cache_plan(const attn_cache_plan_desc* desc)
+{
+    if (!desc) return ATTN_ERR_NULL_PTR;
+    if (desc->struct_size != sizeof(attn_cache_plan_desc)) return ATTN_ERR_ABI;
+    const attn_cache_plan_desc& d = *desc;
+    CachePlanParams p = {};
+    p.bshift = block_shift(d.block_size);
+    if (p.bshift < 0) return ATTN_ERR_UNSUPPORTED;
+    if (d.batch < 0 || d.table_width < 0 || d.free_len < 0 || d.total_new < 0 || d.stride_table < 0)
+        return ATTN_ERR_BAD_SHAPE;
+    if (d.total_new > kInt32Max) return ATTN_ERR_UNSUPPORTED;
+    p.stride_table = d.stride_table ? d.stride_table : d.table_width;
+    if (d.batch > 1 && p.stride_table < d.table_width) return ATTN_ERR_BAD_SHAPE;
+    if (d.flags & ~ATTN_FLAG_LOG) return ATTN_ERR_BAD_VARIANT;
+    if (!d.num_free || !d.num_free_out || !d.cu_seqlens_q) return ATTN_ERR_NULL_PTR;
+    if (d.batch > 0 && (!d.cached_lens || !d.new_lens || !d.seqlens_k)) return ATTN_ERR_NULL_PTR;
+    if (d.batch > 0 && d.table_width > 0 && !d.block_tables) return ATTN_ERR_NULL_PTR;
+    if ((d.free_len > 0 && !d.free_blocks) || (d.total_new > 0 && !d.slots)) return ATTN_ERR_NULL_PTR;
+    if (d.num_free_out == d.num_free) return ATTN_ERR_BAD_SHAPE;  // read by every workgroup
+    for (const void* q : {(const void*)d.cached_lens, (const void*)d.new_lens, (const void*)d.block_tables,
+                          (const void*)d.free_blocks, (const void*)d.num_free, (const void*)d.cu_seqlens_q,
+                          (const void*)d.seqlens_k, (const void*)d.num_free_out})
+        if (!aligned(q, 4)) return ATTN_ERR_ALIGNMENT;
+    if (!aligned(d.slots, 8)) return ATTN_ERR_ALIGNMENT;
+    p.cached = d.cached_lens;
+    p.fresh = d.new_lens;
+    p.table = d.block_tables;
+    p.free_blocks = d.free_blocks;
+    p.num_free = d.num_free;
+    p.slots = d.slots;
+    p.cu = d.cu_seqlens_q;
+    p.seqlens = d.seqlens_k;
+    p.num_free_out = d.num_free_out;
+    p.total_new = d.total_new;
+    p.batch = d.batch;
+    p.width = d.table_width;
+    p.free_len = d.free_len;
+    if (d.flags & ATTN_FLAG_LOG)
+        std::fprintf(stderr, "attn_cache_plan: B=%d block %d table width %d, %lld new tokens\n", d.batch,
+                     d.block_size, d.table_width, (long long)d.total_new);
+    return launched(attn::launch_cache_plan(p, static_cast<hipStream_t>(d.stream)), d.flags,
+                    "attn_cache_plan");
+}
+
+// ATTN_FLAG_VALIDATE of attn_cache_append: one run of ascending places per block.
+static int validate_slots(const attn_cache_append_desc& d, int64_t num_slots, int bshift)
+{
+    std::vector<int64_t> s;
+    if (!fetch(d.slots, d.total_new, static_cast<hipStream_t>(d.stream), &s)) return ATTN_ERR_LAUNCH;
+    std::unordered_set<int64_t> seen;
+    int64_t before = -1;  // the slot before, -1 where it names none
+    for (int64_t x : s) {
+        if (x < 0 || x >= num_slots) {
+            before = -1;
+            continue;
+        }
+        if (before >= 0 && x >> bshift == before >> bshift) {
+            if (x != before + 1) return ATTN_ERR_BAD_SHAPE;
+        } else if (!seen.insert(x >> bshift).second) {
+            return ATTN_ERR_BAD_SHAPE;
+        }
+        before = x;
+    }
+    return ATTN_OK;
+}
+
+extern "C" int attn_cache_append(const void* k, const void* v, const attn_cache* cache,
+                                 const attn_cache_append_desc* desc)
+{
+    if (!desc) return ATTN_ERR_NULL_PTR;
+    if (desc->struct_size != sizeof(attn_cache_append_desc)) return ATTN_ERR_ABI;
+    const attn_cache_append_desc& d = *desc;
+    CacheAppendParams p = {};
+    int rc = check_cache(cache, &p.pool);
+    if (rc != ATTN_OK) return rc;
+    if (d.dtype != ATTN_BF16 && d.dtype != ATTN_FP32) return ATTN_ERR_UNSUPPORTED;
+    if (d.total_new < 0) return ATTN_ERR_BAD_SHAPE;
+    if (d.total_new > kInt32Max) return ATTN_ERR_UNSUPPORTED;
+    if (bad_flags(d.flags)) return ATTN_ERR_BAD_VARIANT;
+    const int64_t align = d.dtype == ATTN_BF16 ? 8 : 4, D = cache->head_dim;
+    const int64_t in[4] = {d.stride_k_h, d.stride_v_h, d.stride_k_s, d.stride_v_s};
+    int64_t out[4];
+    for (int i = 0; i < 4; ++i) {
+        if (in[i] < 0) return ATTN_ERR_BAD_SHAPE;
+        if (in[i] % align) return ATTN_ERR_ALIGNMENT;
+        out[i] = in[i] ? in[i] : i < 2 ? D : cache->num_kv_heads * D;
+    }
+    if (d.total_new == 0) return ATTN_OK;
+    if (!k || !v || !d.slots) return ATTN_ERR_NULL_PTR;
+    rc = check_cache_pointers(cache, &p.pool);
+    if (rc != ATTN_OK) return rc;
+    if (!aligned16(k) || !aligned16(v) || !aligned(d.slots, 8)) return ATTN_ERR_ALIGNMENT;
+    p.x[0] = k;
+    p.x[1] = v;
+    for (int i = 0; i < 2; ++i) {
+        p.sx_h[i] = out[i];
+        p.sx_s[i] = out[2 + i];
+    }
+    p.slots = d.slots;
+    p.total_new = d.total_new;
+    p.num_slots = (int64_t)cache->num_blocks << p.pool.bshift;
+    // 4 tokens a workgroup (a decode step's runs, one for each wavefront), 16 where
+    // that still leaves 2048 workgroups: most of a prompt's start no run.
+    p.group = d.total_new * cache->num_kv_heads * 2 >= 16 * 2048 ? 16 : 4;
+    if (d.flags & ATTN_FLAG_VALIDATE) {
+        rc = validate_slots(d, p.num_slots, p.pool.bshift);
+        if (rc != ATTN_OK) return rc;
+    }
+    if (d.flags & ATTN_FLAG_LOG)
+        std::fprintf(stderr, "attn_cache_append: %s -> %s D=%d Hkv=%d block %d | %lld tokens, %d a workgroup\n",
+                     d.dtype == ATTN_BF16 ? "bf16" : "fp32", format_name(cache), cache->head_dim,
+                     cache->num_kv_heads, cache->block_size, (long long)d.total_new, p.group);
+    return launched(attn::launch_cache_append(p, cache->head_dim, cache->cache_dtype == ATTN_E5M2,
+                                              d.dtype == ATTN_FP32, static_cast<hipStream_t>(d.stream)),
+                    d.flags, "attn_cache_append");
+}
+
+namespace {
+
+struct FwdShape {
+    CacheFwdKind kind;
+    int64_t max_q;  // longest query length; 0: nothing to compute
+};
+
+int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdParams& p, FwdShape* s)
+{
+    int rc = check_cache(cache, &p.pool);
+    if (rc != ATTN_OK) return rc;
+    if (d.dtype != ATTN_BF16 && d.dtype != ATTN_FP32) return ATTN_ERR_UNSUPPORTED;
+    if (d.batch < 0 || d.num_q_heads <= 0 || d.num_q_heads % cache->num_kv_heads != 0)
+        return ATTN_ERR_BAD_SHAPE;
+    if (d.mask_kind != ATTN_MASK_NONE && d.mask_kind != ATTN_MASK_CAUSAL &&
+        d.mask_kind != ATTN_MASK_SLIDING_WINDOW)
+        return d.mask_kind >= ATTN_MASK_PREFIX_LM && d.mask_kind <= ATTN_MASK_CAUSAL_BLOCKWISE
+                   ? ATTN_ERR_UNSUPPORTED
+                   : ATTN_ERR_BAD_VARIANT;
+    if (d.mask_kind == ATTN_MASK_SLIDING_WINDOW && (d.window_left < -1 || d.window_right < -1))
+        return ATTN_ERR_BAD_VARIANT;
+    if (!std::isfinite(d.scale) || !(d.scale > 0.0f)) return ATTN_ERR_BAD_VARIANT;
+    if (!std::isfinite(d.softcap) || d.softcap < 0.0f) return ATTN_ERR_BAD_VARIANT;
+    if (d.softcap > 0.0f && !std::isfinite(d.scale / d.softcap * (float)(2.0 * 1.4426950408889634)))
+        return ATTN_ERR_BAD_VARIANT;
+    if (bad_flags(d.flags)) return ATTN_ERR_BAD_VARIANT;
+    const bool packed = d.cu_seqlens_q != nullptr;
+    if (packed ? d.max_seqlen_q < 0 || d.total_q < 0 : d.seqlen_q < 0) return ATTN_ERR_BAD_SHAPE;
+    if (d.max_seqlen_k < 0 || d.table_width < 0 || d.stride_table < 0) return ATTN_ERR_BAD_SHAPE;
+    p.stride_table = d.stride_table ? d.stride_table : d.table_width;
+    if (d.batch > 1 && p.stride_table < d.table_width) return ATTN_ERR_BAD_SHAPE;
+    const int64_t max_q = packed ? std::min<int64_t>(d.max_seqlen_q, d.total_q) : d.seqlen_q;
+    const int64_t D = cache->head_dim, align = d.dtype == ATTN_BF16 ? 8 : 4;
+    const int64_t rows = packed ? 0 : max_q;
+    const int64_t in[6] = {d.stride_q_b, d.stride_q_h, d.stride_q_s, d.stride_o_b, d.stride_o_h, d.stride_o_s};
+    int64_t out[6];
+    for (int i = 0; i < 6; ++i) {
+        if (in[i] < 0) return ATTN_ERR_BAD_SHAPE;
+        if (in[i] % align) return ATTN_ERR_ALIGNMENT;
+        const int64_t usual = packed ? (i % 3 == 1 ? D : i % 3 == 2 ? d.num_q_heads * D : 0)
+                                     : (i % 3 == 0   ? d.num_q_heads * rows * D
+                                        : i % 3 == 1 ? rows * D
+                                                     : D);
+        out[i] = in[i] ? in[i] : usual;
+    }
+    p.sq_b = packed ? 0 : out[0], p.sq_h = out[1], p.sq_s = out[2];
+    p.so_b = packed ? 0 : out[3], p.so_h = out[4], p.so_s = out[5];
+
+    p.batch = d.batch;
+    p.hq = d.num_q_heads;
+    p.seqlen_q = packed ? 0 : d.seqlen_q;
+    p.total_q = packed ? d.total_q : 0;
+    p.width = d.table_width;
+    p.wl = d.mask_kind == ATTN_MASK_SLIDING_WINDOW ? d.window_left : -1;
+    p.wr = d.mask_kind == ATTN_MASK_CAUSAL           ? 0
+           : d.mask_kind == ATTN_MASK_SLIDING_WINDOW ? d.window_right
+                                                     : -1;
+    const double log2e = 1.4426950408889634;
+    p.scale_u = (float)(d.scale * log2e);
+    p.cap_pre = d.softcap > 0.0f ? d.scale / d.softcap : 0.0f;
+    p.cap_post = (float)(d.softcap * log2e);
+    const int group = d.num_q_heads / cache->num_kv_heads;
+    p.div_group = make_fastdiv((uint32_t)group);
+    p.div_hkv = make_fastdiv((uint32_t)cache->num_kv_heads);
+    s->max_q = d.batch == 0 ? 0 : max_q;
+    s->kind = {cache->head_dim, cache->cache_dtype == ATTN_E5M2, d.dtype == ATTN_FP32, false};
+    // flat rows and workgroups are numbered with 31 bits
+    const int64_t most = packed ? d.total_q : max_q;
+    if (most * group > kInt32Max || (int64_t)d.batch * d.num_q_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
+    // Flat rows of a request at most: few of them share 16-row tiles whose keys are
+    // split over wavefronts, many take 128-row tiles.
+    const int64_t flat = s->max_q * group;
+    s->kind.many_rows = flat > 64;
+    p.tile_rows = attn::cache_tile_rows(s->kind);
+    const int64_t row_tiles = (flat + p.tile_rows - 1) / p.tile_rows;
+    if (row_tiles * d.batch * cache->num_kv_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
+    p.row_tiles = (int32_t)row_tiles;
+    return ATTN_OK;
+}
+
+int64_t part_rows(const CacheFwdParams& p, int64_t splits)
+{
+    return (int64_t)p.batch * p.pool.hkv * p.row_tiles * splits * p.tile_rows;
+}
+
+int64_t workspace_need(const CacheFwdParams& p, int64_t D)
+{
+    return p.splits > 1 ? part_rows(p, p.splits) * (D + 2) * (int64_t)sizeof(float) : 0;
+}
+
+// Key splits: enough workgroups for the chip's slots (three workgroups of few
+// rows fit a CU, two of many), each with a few chunks for each of its wavefronts,
+// within the workspace's limit (a quarter of the bytes of q, out, K and V, or
+// 64 MiB where that is more).
+void plan_splits(const attn_cache_fwd_desc& d, const FwdShape& s, CacheFwdParams& p)
+{
+    const int64_t D = s.kind.head_dim, items = (int64_t)p.batch * p.pool.hkv * p.row_tiles;
+    int64_t keys = (int64_t)p.width << p.pool.bshift;
+    if (d.max_seqlen_k > 0) keys = std::min<int64_t>(keys, d.max_seqlen_k);
+    const int64_t span = std::min<int64_t>(p.tile_rows / (int64_t)p.div_group.d + 2, s.max_q);
+    if (p.wl >= 0 && p.wr >= 0) keys = std::min<int64_t>(keys, (int64_t)p.wl + p.wr + span);
+    const int64_t chunks = keys / kChunkKeys + 2;
+    const int64_t slots = s.kind.many_rows ? 512 : 768, least = 8;
+    int64_t splits = std::min({(slots + items - 1) / items, (chunks + least - 1) / least, kMaxSplits});
+    const int64_t elt = s.kind.fp32 ? 4 : 2;
+    const int64_t rows = d.cu_seqlens_q ? d.total_q : (int64_t)d.batch * d.seqlen_q;
+    const int64_t bytes = 2 * D * (rows * p.hq * elt + keys * p.batch * p.pool.hkv);
+    const int64_t limit = std::max<int64_t>(bytes / 4, (int64_t)64 << 20);
+    splits = std::min(splits, limit / (part_rows(p, 1) * (D + 2) * (int64_t)sizeof(float)));
+    p.splits = (int32_t)std::max<int64_t>(splits, 1);
+    p.split_chunks = (int32_t)std::max((chunks + p.splits - 1) / p.splits, least);
+}
+
+void no_splits(CacheFwdParams& p)
+{
+    p.splits = 1;
+    p.split_chunks = 1 << 30;
+}
+
+int validate_fwd(const attn_cache_fwd_desc& d, const CacheFwdParams& p, int64_t max_q)
+{
+    hipStream_t stream = static_cast<hipStream_t>(d.stream);
+    std::vector<int32_t> cu, lens, row;
+    if (d.cu_seqlens_q) {
+        if (!fetch(d.cu_seqlens_q, (int64_t)d.batch + 1, stream, &cu)) return ATTN_ERR_LAUNCH;
+        if (cu[0] < 0 || cu[(size_t)d.batch] > d.total_q) return ATTN_ERR_BAD_SHAPE;
+        for (int32_t b = 0; b < d.batch; ++b) {
+            const int64_t n = (int64_t)cu[(size_t)b + 1] - cu[(size_t)b];
+            if (n < 0 || n > max_q) return ATTN_ERR_BAD_SHAPE;
+        }
+    }
+    if (!fetch(d.seqlens_k, d.batch, stream, &lens)) return ATTN_ERR_LAUNCH;
+    for (int32_t b = 0; b < d.batch; ++b) {
+        const int64_t n = lens[(size_t)b];
+        if (n < 0 || n > (int64_t)p.width << p.pool.bshift) return ATTN_ERR_BAD_SHAPE;
+        const int64_t used = (n + (1 << p.pool.bshift) - 1) >> p.pool.bshift;
+        if (!fetch(d.block_tables + b * p.stride_table, used, stream, &row)) return ATTN_ERR_LAUNCH;
+        // (entries behind a window's left end may have been given back)
+        const int64_t lq = d.cu_seqlens_q ? (int64_t)cu[(size_t)b + 1] - cu[(size_t)b] : d.seqlen_q;
+        const int64_t lo = p.wl < 0 ? 0 : std::max<int64_t>(n - lq - p.wl, 0);
+        for (int64_t i = lo >> p.pool.bshift; i < used; ++i)
+            if (row[(size_t)i] < 0 || row[(size_t)i] >= p.pool.num_blocks) return ATTN_ERR_BAD_VARIANT;
+    }
+    return ATTN_OK;
+}
+
+}  // namespace
+
+extern "C" int64_t attn_cache_workspace_bytes(const attn_cache* cache, const attn_cache_fwd_desc* desc)
+{
+    if (!desc) return ATTN_ERR_NULL_PTR;
+    if (desc->struct_size != sizeof(attn_cache_fwd_desc)) return ATTN_ERR_ABI;
+    CacheFwdParams p = {};
+    FwdShape s;
+    const int rc = check_fwd(cache, *desc, p, &s);
+    if (rc != ATTN_OK) return rc;
+    if (s.max_q == 0) return 0;
+    plan_splits(*desc, s, p);
+    return workspace_need(p, s.kind.head_dim);
+}
+
+extern "C" int attn_cache_fwd(const void* q, void* out, float* lse, const attn_cache* cache,
+                              const attn_cache_fwd_desc* desc, void* workspace, int64_t workspace_bytes)
+{
+    if (!desc) return ATTN_ERR_NULL_PTR;
+    if (desc->struct_size != sizeof(attn_cache_fwd_desc)) return ATTN_ERR_ABI;
+    const attn_cache_fwd_desc& d = *desc;
+    CacheFwdParams p = {};
+    FwdShape s;
+    int rc = check_fwd(cache, d, p, &s);
+    if (rc != ATTN_OK) return rc;
+    if (s.max_q == 0) return ATTN_OK;  // nothing to compute
+    if (!q || !out || !d.seqlens_k || (d.table_width > 0 && !d.block_tables)) return ATTN_ERR_NULL_PTR;
+    rc = check_cache_pointers(cache, &p.pool);
+    if (rc != ATTN_OK) return rc;
+    const bool packed = d.cu_seqlens_q != nullptr;
+    {
+        const int64_t size[3] = {packed ? d.total_q : d.batch, d.num_q_heads, packed ? 1 : d.seqlen_q};
+        const int64_t stride[3] = {packed ? p.so_s : p.so_b, p.so_h, p.so_s};
+        if (!rows_disjoint(s.kind.head_dim, 3, size, stride)) return ATTN_ERR_BAD_SHAPE;
+    }
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return ATTN_ERR_ALIGNMENT;
+    for (const void* a : {(const void*)lse, (const void*)d.block_tables, (const void*)d.seqlens_k,
+                          (const void*)d.cu_seqlens_q, (const void*)d.alibi_slopes})
+        if (!aligned(a, 4)) return ATTN_ERR_ALIGNMENT;
+    p.q = q;
+    p.o = out;
+    p.lse = lse;
+    p.slopes = d.alibi_slopes;
+    p.table = d.block_tables;
+    p.seqlens = d.seqlens_k;
+    p.cu_q = d.cu_seqlens_q;
+    plan_splits(d, s, p);
+    const int64_t need = workspace_need(p, s.kind.head_dim);
+    if (need > 0 && workspace && workspace_bytes >= need) {
+        p.ws_o = static_cast<float*>(workspace);
+        p.ws_ml = p.ws_o + part_rows(p, p.splits) * s.kind.head_dim;
+    } else {
+        no_splits(p);
+    }
+    if (d.flags & ATTN_FLAG_VALIDATE) {
+        rc = validate_fwd(d, p, s.max_q);
+        if (rc != ATTN_OK) return rc;
+    }
+    if (d.flags & ATTN_FLAG_LOG)
+        std::fprintf(stderr,
+                     "attn_cache_fwd: %s over %s D=%d B=%d Hq=%d Hkv=%d block %d %s window (%d, %d) alibi=%d "
+                     "softcap=%g | %s rows, %d a tile, %d tiles a kv head, key splits %d\n",
+                     s.kind.fp32 ? "fp32" : "bf16", format_name(cache), s.kind.head_dim, d.batch, d.num_q_heads,
+                     p.pool.hkv, cache->block_size, packed ? "packed" : "fixed-length", p.wl, p.wr,
+                     p.slopes != nullptr, (double)d.softcap, s.kind.many_rows ? "many" : "few", p.tile_rows,
+                     p.row_tiles, p.splits);
+    hipStream_t stream = static_cast<hipStream_t>(d.stream);
+    hipError_t err = attn::launch_cache_fwd(p, s.kind, stream);
+    if (err == hipSuccess && p.splits > 1) err = attn::launch_cache_combine(p, s.kind, stream);
+    return launched(err, d.flags, "attn_cache_fwd");
+}

@@ -1,0 +1,455 @@
+// cache_kernel.h -- softmax attention to an 8-bit block cache: the kernel that
+// cache_fwd_*.hip instantiate.
+//
+// A wavefront takes 64 consecutive keys at a time against MT tiles of 16 flat
+// rows (row f of a kv group: query f / group of head f % group, so K and V are
+// read once for all the heads that use them), entirely in registers:
+//  * S^T = K Q^T with v_mfma_f32_16x16x32_bf16. Row m of product tile t stands
+//    for key 16 (m / 4) + 4 t + m % 4 of the 64, so that the sixteen scores a
+//    lane holds of a row (lanes r, r + 16, r + 32, r + 48 share row r) belong to
+//    sixteen consecutive keys, 16 g on for g = lane / 16: one page, one scale.
+//    The head dim is taken in the order of the loads: a lane's 16 bytes feed two
+//    products.
+//  * O^T = V^T P^T: those sixteen keys are, as they stand, the lane's share of the
+//    B operand, and V, stored transposed, gives the A operand in one 16-byte
+//    load per 16 dims. No value of K, V or P passes through LDS or another lane.
+//  * 8-bit values become bf16 exactly (both formats have fewer mantissa bits);
+//    the scale of a block multiplies the score, that of V the probability,
+//    both in fp32. For fp32 calls q and P are split into three bf16 terms (24
+//    bits), each with products of its own into the same sums.
+// Few rows: the wavefronts of a workgroup take every fourth chunk of 64 keys and
+// are merged through LDS, and the keys are split over workgroups. Many rows:
+// they take row tiles of their own.
+#pragma once
+
+#include "cache_params.h"
+#include "kernel_params.h"
+#include "score_mods.h"
+
+namespace attn {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int NT = 256, kWaves = 4;
+constexpr int kChunk = 64;  // keys a wavefront takes at a time
+
+// A row tile of one kv group and the keys its rows see.
+struct RowTile {
+    int b, hkv, f0, nflat;   // nflat: flat rows of the kv group
+    int64_t qrow0;           // packed: first row of the request
+    int64_t lk, lq;          // lengths that place the queries on the key axis
+    int64_t kend;            // keys the table holds
+};
+
+// Visible keys [lo, hi) of query qi (hi <= lo: none).
+__device__ __forceinline__ void row_keys(const CacheFwdParams& p, const RowTile& t, int64_t qi, int64_t* lo,
+                                         int64_t* hi)
+{
+    const int64_t ip = qi + t.lk - t.lq;
+    *lo = p.wl < 0 ? 0 : max(ip - p.wl, (int64_t)0);
+    *hi = p.wr < 0 ? t.kend : min(t.kend, ip + p.wr + 1);
+}
+
+// false: a tile without rows.
+__device__ __forceinline__ bool row_tile(const CacheFwdParams& p, uint32_t g, uint32_t rt, RowTile* t)
+{
+    t->b = (int)fast_div(g, p.div_hkv);
+    t->hkv = (int)g - t->b * p.pool.hkv;
+    t->qrow0 = 0;
+    t->lq = p.seqlen_q;
+    if (p.cu_q) {
+        // (limits for prefix sums that are none: no row outside q and out)
+        t->qrow0 = min(max((int64_t)p.cu_q[t->b], (int64_t)0), p.total_q);
+        t->lq = max(min((int64_t)p.cu_q[t->b + 1], p.total_q) - t->qrow0, (int64_t)0);
+    }
+    t->lk = max(p.seqlens[t->b], 0);
+    t->kend = min(t->lk, (int64_t)p.width << p.pool.bshift);
+    t->nflat = (int)(t->lq * p.div_group.d);
+    t->f0 = (int)rt * p.tile_rows;
+    return t->f0 < t->nflat;
+}
+
+// Chunks [c0, c1) that rows [f0, f0 + n) of the tile see, and how many splits
+// share them (0: one at most, which writes the output itself).
+__device__ __forceinline__ void tile_chunks(const CacheFwdParams& p, const RowTile& t, int f0, int n, int* c0,
+                                            int* c1)
+{
+    const int q0 = (int)fast_div((uint32_t)f0, p.div_group);
+    const int q1 = (int)fast_div((uint32_t)min(f0 + n, t.nflat) - 1u, p.div_group);
+    int64_t lo, hi, none;
+    row_keys(p, t, q0, &lo, &none);
+    row_keys(p, t, q1, &none, &hi);
+    *c0 = (int)(lo / kChunk);
+    *c1 = hi > lo ? (int)((hi + kChunk - 1) / kChunk) : *c0;
+}
+
+__device__ __forceinline__ int split_size(const CacheFwdParams& p, int chunks)
+{
+    return max(p.split_chunks, (chunks + p.splits - 1) / p.splits);
+}
+
+// Work item -> (kv group, row tile): the row tiles of a group follow one another
+// and, when the groups are a multiple of eight, on one XCD (ids are dealt
+// round-robin over the 8 XCDs), so that they meet in its L2.
+__device__ __forceinline__ void work_item(const CacheFwdParams& p, uint32_t id, uint32_t* g, uint32_t* rt)
+{
+    const uint32_t groups = (uint32_t)(p.batch * p.pool.hkv), nrt = (uint32_t)p.row_tiles;
+    if (groups % 8 == 0) {
+        const uint32_t k = id >> 3;
+        *rt = k % nrt;
+        *g = (id & 7) + 8 * (k / nrt);
+    } else {
+        *rt = id % nrt;
+        *g = id / nrt;
+    }
+}
+
+template <bool E5M2, bool HI>
+__device__ __forceinline__ bf16x2 to_bf16(uint32_t w)
+{
+    if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, HI);
+    else return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI);
+}
+
+template <bool E5M2>
+__device__ __forceinline__ bf16x8 to_bf16x8(uint32_t a, uint32_t b)
+{
+    const bf16x2 w0 = to_bf16<E5M2, false>(a), w1 = to_bf16<E5M2, true>(a);
+    const bf16x2 w2 = to_bf16<E5M2, false>(b), w3 = to_bf16<E5M2, true>(b);
+    return bf16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
+}
+
+// Sum and maximum over the lanes that share a row (lane mod 16).
+__device__ __forceinline__ float row_max(float x)
+{
+    x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+    return __builtin_fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// The bytes of dword i of a lane's sixteen keys that lie in [lo, hi).
+__device__ __forceinline__ uint32_t byte_mask(int i, int lo, int hi)
+{
+    const int a = min(max(lo - 4 * i, 0), 4), b = min(max(hi - 4 * i, 0), 4);
+    const uint32_t below_b = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+    const uint32_t below_a = a == 4 ? ~0u : (1u << (8 * a)) - 1u;
+    return below_b & ~below_a;
+}
+
+// O, row sum and maximum of one row (lane: 4 consecutive dims) to the output,
+// or to the partials of split sp.
+template <int D, class T>
+struct Writer {
+    const CacheFwdParams& p;
+    const RowTile& t;
+    int64_t part;  // index of the tile's first partial row, or -1
+
+    __device__ __forceinline__ void scalars(int f, int row, float m, float l) const
+    {
+        if (part >= 0) {
+            p.ws_ml[2 * (part + row)] = m;
+            p.ws_ml[2 * (part + row) + 1] = l;
+        } else if (p.lse) {
+            const int qi = (int)fast_div((uint32_t)f, p.div_group);
+            const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
+            const int64_t at = p.cu_q ? h * p.total_q + t.qrow0 + qi
+                                      : ((int64_t)t.b * p.hq + h) * p.seqlen_q + qi;
+            p.lse[at] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+        }
+    }
+    __device__ __forceinline__ float factor(float l) const  // (a NaN sum reaches O)
+    {
+        return part >= 0 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+    }
+    __device__ __forceinline__ void out(int f, int row, int d, f32x4 x) const
+    {
+        if (part >= 0) {
+            *reinterpret_cast<f32x4*>(p.ws_o + (part + row) * D + d) = x;
+            return;
+        }
+        const int qi = (int)fast_div((uint32_t)f, p.div_group);
+        const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
+        T* dst = static_cast<T*>(p.o) + (p.cu_q ? t.qrow0 + qi : qi) * p.so_s + h * p.so_h +
+                 (p.cu_q ? 0 : t.b * p.so_b) + d;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<bf16x4*>(dst) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        else
+            *reinterpret_cast<f32x4*>(dst) = x;
+    }
+};
+
+// T: element of q and out. MODS: soft-cap or ALiBi (one instantiation for both:
+// the vector work beside them is the conversion of K and V).
+template <int D, class T, bool E5M2, int MT, bool MODS, bool MANY>
+__global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
+{
+    constexpr int NS = sizeof(T) == 2 ? 1 : 3;  // bf16 terms of q and P
+    constexpr int WR = 16 * MT;                 // rows of a wavefront
+    constexpr int KS = D / 32, DT = D / 16;     // products along the head dim, tiles of it
+    constexpr int HV = D / 64;                  // 16-byte loads of a key row per lane
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+
+    uint32_t group, rt;
+    work_item(p, blockIdx.x, &group, &rt);
+    RowTile t;
+    if (!row_tile(p, group, rt, &t)) return;  // whole workgroup
+    int c0, c1;
+    tile_chunks(p, t, t.f0, p.tile_rows, &c0, &c1);
+    const int sp = blockIdx.y, per = split_size(p, c1 - c0);
+    const bool split = c1 - c0 > per;
+    if (sp > 0 && c0 + sp * per >= c1) return;  // whole workgroup
+    c0 += sp * per;
+    c1 = min(c1, c0 + per);
+    const int64_t part =
+        split ? (((int64_t)group * p.row_tiles + rt) * p.splits + sp) * p.tile_rows : (int64_t)-1;
+    const Writer<D, T> write{p, t, part};
+
+    const int fw = t.f0 + (MANY ? wave * WR : 0);  // the wavefront's first row
+    if (MANY && fw >= t.nflat) return;             // (no barrier under MANY)
+    // keys that any, and that every row of the wavefront sees
+    int64_t lo_any, hi_any, lo_all, hi_all;
+    {
+        const int q0 = (int)fast_div((uint32_t)fw, p.div_group);
+        const int q1 = (int)fast_div((uint32_t)min(fw + WR, t.nflat) - 1u, p.div_group);
+        row_keys(p, t, q0, &lo_any, &hi_all);
+        row_keys(p, t, q1, &lo_all, &hi_any);
+        if (MANY) {
+            c0 = max(c0, (int)(lo_any / kChunk));
+            c1 = hi_any > lo_any ? min(c1, (int)((hi_any + kChunk - 1) / kChunk)) : c0;
+        }
+    }
+
+    // q: lane holds dims 64 h + 16 g + 8 e .. + 7 of its row for product 2 h + e
+    bf16x8 qf[MT][KS][NS];
+    int64_t jlo[MT], jhi[MT];
+    int64_t ip[MT];
+    float slope[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int f = min(fw + 16 * m + r, t.nflat - 1);
+        const int qi = (int)fast_div((uint32_t)f, p.div_group);
+        const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
+        row_keys(p, t, qi, &jlo[m], &jhi[m]);
+        ip[m] = qi + t.lk - t.lq;
+        slope[m] = MODS && p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
+        const T* src = static_cast<const T*>(p.q) + (p.cu_q ? t.qrow0 + qi : qi) * p.sq_s + h * p.sq_h +
+                       (p.cu_q ? 0 : t.b * p.sq_b) + 16 * g;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const T* s = src + 64 * (k / 2) + 8 * (k % 2);
+            if constexpr (NS == 1) {
+                qf[m][k][0] = *reinterpret_cast<const bf16x8*>(s);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = s[e];
+                    const __bf16 a = (__bf16)x, b = (__bf16)(x - (float)a);
+                    qf[m][k][0][e] = a;
+                    qf[m][k][1][e] = b;
+                    qf[m][k][2][e] = (__bf16)(x - (float)a - (float)b);
+                }
+            }
+        }
+    }
+
+    f32x4 acc[MT][DT];
+    float mx[MT], sum[MT];  // running maximum of the row; this lane's share of the sum
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        mx[m] = -__builtin_inff();
+        sum[m] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[m][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const int bshift = p.pool.bshift, bs1 = (1 << bshift) - 1;
+    const int32_t* table = p.table + t.b * p.stride_table;
+    // page of the 16 keys from key16 on; -1 where no row sees any or the entry is bad
+    auto page_of = [&](int64_t key16) __attribute__((always_inline)) -> int {
+        if (key16 >= hi_any || key16 + 16 <= lo_any) return -1;
+        const int page = table[key16 >> bshift];
+        return (uint32_t)page < (uint32_t)p.pool.num_blocks ? page : -1;
+    };
+
+    for (int c = c0 + (MANY ? 0 : wave); c < c1; c += MANY ? 1 : kWaves) {
+        const int64_t base = (int64_t)c * kChunk;
+        const int64_t key_k = base + 16 * (r >> 2), key_v = base + 16 * g;
+        const int page_k = page_of(key_k), page_v = page_of(key_v);
+        // (a page that is not there: block 0 is read and masked out)
+        const uint8_t* kp = p.pool.k + (int64_t)max(page_k, 0) * p.pool.sk_b + t.hkv * p.pool.sk_h +
+                            (((int)key_k & bs1) + (r & 3)) * D + 16 * g;
+        const uint8_t* vp = p.pool.v + (int64_t)max(page_v, 0) * p.pool.sv_b + t.hkv * p.pool.sv_h +
+                            (r << bshift) + ((int)key_v & bs1);
+        u32x4 kw[4][HV], vw[DT];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int h = 0; h < HV; ++h) kw[u][h] = *reinterpret_cast<const u32x4*>(kp + 4 * u * D + 64 * h);
+        const float ks = page_v < 0 ? 0.0f : p.pool.k_scale[page_v * p.pool.sks_b + t.hkv];
+        const float vs = page_v < 0 ? 0.0f : p.pool.v_scale[page_v * p.pool.svs_b + t.hkv];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vw[d] = *reinterpret_cast<const u32x4*>(vp + (d << (4 + bshift)));
+
+        f32x4 s[MT][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) s[m][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const bf16x8 a = to_bf16x8<E5M2>(kw[u][k / 2][2 * (k % 2)], kw[u][k / 2][2 * (k % 2) + 1]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = NS - 1; n >= 0; --n) s[m][u] = mfma(a, qf[m][k][n], s[m][u]);
+            }
+        }
+
+        // whole: every row sees all 64 keys, in pages that are there
+        const bool whole = base >= lo_all && base + kChunk <= hi_all &&
+                           __builtin_amdgcn_ballot_w64(page_v < 0) == 0;
+        if (!whole) {
+            // bytes of V that no row sees weigh 0, whatever they hold
+            const int lo = (int)min(max(lo_any - key_v, (int64_t)0), (int64_t)16);
+            const int hi = page_v < 0 ? 0 : (int)min(max(hi_any - key_v, (int64_t)0), (int64_t)16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t keep = byte_mask(i, lo, hi);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) vw[d][i] &= keep;
+            }
+        }
+
+        bf16x8 pf[MT][2][NS];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float x[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float dot = s[m][j / 4][j % 4] * ks;
+                if constexpr (MODS) {
+                    x[j] = p.cap_post != 0.0f ? softcap_u(dot, p.cap_pre, p.cap_post) : dot * p.scale_u;
+                    x[j] = __builtin_fmaf(slope[m], __builtin_fabsf((float)(int)(ip[m] - key_v - j)), x[j]);
+                } else {
+                    x[j] = dot * p.scale_u;
+                }
+            }
+            if (!whole) {
+                const int lo = (int)min(max(jlo[m] - key_v, (int64_t)0), (int64_t)16);
+                const int hi = page_v < 0 ? 0 : (int)min(max(jhi[m] - key_v, (int64_t)0), (int64_t)16);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) x[j] = j >= lo && j < hi ? x[j] : -__builtin_inff();
+            }
+            float top = x[0];
+#pragma unroll
+            for (int j = 1; j < 16; ++j) top = __builtin_fmaxf(top, x[j]);
+            const float now = __builtin_fmaxf(mx[m], row_max(top));
+            // a row that has seen no key yet: exponents of 0 - inf, not inf - inf
+            const float ref = now == -__builtin_inff() ? 0.0f : now;
+            const float keep = __builtin_amdgcn_exp2f(mx[m] - ref);
+            mx[m] = now;
+            float add = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float e = __builtin_amdgcn_exp2f(x[j] - ref);
+                add += e;
+                const float w = e * vs;
+                const __bf16 a = (__bf16)w;
+                pf[m][j / 8][0][j % 8] = a;
+                if constexpr (NS == 3) {
+                    const __bf16 b = (__bf16)(w - (float)a);
+                    pf[m][j / 8][1][j % 8] = b;
+                    pf[m][j / 8][2][j % 8] = (__bf16)(w - (float)a - (float)b);
+                }
+            }
+            sum[m] = __builtin_fmaf(sum[m], keep, add);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[m][d] *= keep;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 a = to_bf16x8<E5M2>(vw[d][2 * k], vw[d][2 * k + 1]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = NS - 1; n >= 0; --n) acc[m][d] = mfma(a, pf[m][k][n], acc[m][d]);
+            }
+    }
+
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sum[m] = row_sum(sum[m]);
+    if constexpr (MANY) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int f = fw + 16 * m + r;
+            if (f >= t.nflat) continue;
+            const float inv = write.factor(sum[m]);
+            if (g == 0) write.scalars(f, f - t.f0, mx[m], sum[m]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) write.out(f, f - t.f0, 16 * d + 4 * g, acc[m][d] * inv);
+        }
+    } else {
+        // merge the wavefronts: every row's O, maximum and sum through LDS (rows of
+        // D + 4 floats: the lanes of a quarter wave write 16 rows to other banks)
+        constexpr int LD = D + 4;
+        __shared__ __attribute__((aligned(16))) float lo_[kWaves][WR * LD];
+        __shared__ float lml[kWaves][WR][2];
+        if constexpr (kLdsPoison) {
+            for (int i = threadIdx.x; i < kWaves * WR * LD; i += NT)
+                (&lo_[0][0])[i] = __builtin_bit_cast(float, ~0u);
+            for (int i = threadIdx.x; i < kWaves * WR * 2; i += NT)
+                (&lml[0][0][0])[i] = __builtin_bit_cast(float, ~0u);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (g == 0) {
+                lml[wave][16 * m + r][0] = mx[m];
+                lml[wave][16 * m + r][1] = sum[m];
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                *reinterpret_cast<f32x4*>(&lo_[wave][(16 * m + r) * LD + 16 * d + 4 * g]) = acc[m][d];
+        }
+        __syncthreads();
+        constexpr int COLS = D / 4;
+        for (int i = threadIdx.x; i < WR * COLS; i += NT) {
+            const int row = i / COLS, col = 4 * (i % COLS), f = t.f0 + row;
+            if (f >= t.nflat) break;
+            float top = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = __builtin_fmaxf(top, lml[w][row][0]);
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                // (no key seen by any: weight 1 of nothing)
+                const float mw = lml[w][row][0];
+                const float k = mw == top ? 1.0f : __builtin_amdgcn_exp2f(mw - top);
+                l = __builtin_fmaf(lml[w][row][1], k, l);
+                o += *reinterpret_cast<const f32x4*>(&lo_[w][row * LD + col]) * k;
+            }
+            if (col == 0) write.scalars(f, row, top, l);
+            write.out(f, row, col, o * write.factor(l));
+        }
+    }
+}
+
+}  // namespace
+}  // namespace attn

@@ -1,0 +1,42 @@
+// cache_launch.h -- the instantiations of cache_fwd_kernel for one head dim.
+#pragma once
+
+#include "cache_kernel.h"
+
+namespace attn {
+namespace {
+
+// Row tiles per wavefront: one for few rows (a decode step fills no more), two
+// for many, which halves the reads and conversions of K and V a row.
+constexpr int kManyTiles = 2;
+
+template <int D, class T, bool E5M2, bool MODS>
+hipError_t launch_rows(const CacheFwdParams& p, bool many, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(p.batch * p.pool.hkv) * (unsigned)p.row_tiles, (unsigned)p.splits);
+    if (many)
+        hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, kManyTiles, MODS, true>), grid, dim3(NT), 0, stream, p);
+    else
+        hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, 1, MODS, false>), grid, dim3(NT), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <int D, class T, bool E5M2>
+hipError_t launch_mods(const CacheFwdParams& p, bool many, hipStream_t stream)
+{
+    return p.slopes || p.cap_post != 0.0f ? launch_rows<D, T, E5M2, true>(p, many, stream)
+                                          : launch_rows<D, T, E5M2, false>(p, many, stream);
+}
+
+template <int D>
+hipError_t launch_head_dim(const CacheFwdParams& p, const CacheFwdKind& k, hipStream_t stream)
+{
+    if (k.fp32)
+        return k.e5m2 ? launch_mods<D, float, true>(p, k.many_rows, stream)
+                      : launch_mods<D, float, false>(p, k.many_rows, stream);
+    return k.e5m2 ? launch_mods<D, __bf16, true>(p, k.many_rows, stream)
+                  : launch_mods<D, __bf16, false>(p, k.many_rows, stream);
+}
+
+}  // namespace
+}  // namespace attn
