@@ -24,6 +24,7 @@ from ._abi import (ATTN_BF16, ATTN_FLAG_LOG, ATTN_FLAG_VALIDATE, ATTN_FP32, ATTN
                    ATTN_MASK_PREFIX_LM, ATTN_MASK_SHARE_QUESTION, ATTN_MASK_SLIDING_WINDOW,
                    ATTN_MAX_SEGMENTS, ATTN_NORM_RELU, ATTN_NORM_SIGMOID, ATTN_NORM_SOFTMAX,
                    AttnError, AttnVariantDesc, check, load, plan_tiles, row_range)
+from . import cache as _cache
 from .cache import (CachePlan, KVCache, cache_append, cache_fwd, cache_plan,  # noqa: F401
                     new_cache)
 
@@ -57,6 +58,7 @@ def _load_native():
                           "paper_2605_05023_amd.build`") from e
     _fast.bind(ctypes.cast(lib.attn_fwd_ws, ctypes.c_void_p).value,
                ctypes.cast(lib.attn_workspace_bytes, ctypes.c_void_p).value)
+    _cache.bind_native(_fast, lib)
     _native = _fast
     return _fast
 

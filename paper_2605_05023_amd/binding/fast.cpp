@@ -15,90 +15,17 @@
 // included) returns NotImplemented before any work, and the Python path of
 // fwd, which raises the errors, runs instead. A launch that fails is raised
 // here: the call is not made a second time. No arithmetic is done here.
-#include <ATen/ATen.h>
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <Python.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <cmath>
-
-#include "../../include/attn.h"
+#include "marshal.h"
 
 namespace {
+
+using namespace attn_py;
 
 using fwd_ws_t = int (*)(const void*, const void*, const void*, void*, float*, const attn_variant_desc*,
                          void*, int64_t);
 using ws_bytes_t = int64_t (*)(const attn_variant_desc*);
 fwd_ws_t g_fwd_ws = nullptr;
 ws_bytes_t g_ws_bytes = nullptr;
-
-// A plain device tensor: no subclass, no functional transform, no lazy bit.
-bool plain(PyObject* o, at::Tensor* t)
-{
-    if (!THPVariable_CheckExact(o)) return false;
-    *t = THPVariable_Unpack(o);
-    if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided) return false;
-    using c10::DispatchKey;
-    const c10::DispatchKeySet odd({DispatchKey::Python, DispatchKey::Functionalize, DispatchKey::Conjugate,
-                                   DispatchKey::Negative, DispatchKey::ZeroTensor,
-                                   DispatchKey::FuncTorchBatched, DispatchKey::FuncTorchGradWrapper});
-    return !t->key_set().has_any(odd);
-}
-
-// An axis of more than one entry with stride 0 (an expanded tensor): the
-// descriptor takes a stride of 0 for the contiguous default.
-bool broadcast(const at::Tensor& t)
-{
-    for (int64_t i = 0; i < t.dim(); ++i)
-        if (t.stride(i) == 0 && t.size(i) > 1) return true;
-    return false;
-}
-
-bool as_int(PyObject* o, int64_t* v)
-{
-    if (!PyLong_CheckExact(o)) return false;
-    int overflow = 0;
-    *v = PyLong_AsLongLongAndOverflow(o, &overflow);
-    return overflow == 0;
-}
-
-bool as_i32(PyObject* o, int32_t* v)
-{
-    int64_t x;
-    if (!as_int(o, &x) || x < INT32_MIN || x > INT32_MAX) return false;
-    *v = (int32_t)x;
-    return true;
-}
-
-bool as_float(PyObject* o, float* v)
-{
-    if (PyFloat_CheckExact(o)) {
-        *v = (float)PyFloat_AS_DOUBLE(o);
-        return true;
-    }
-    int32_t i;
-    if (!as_i32(o, &i)) return false;
-    *v = (float)i;
-    return true;
-}
-
-bool is(PyObject* o, const char* s) { return PyUnicode_CompareWithASCIIString(o, s) == 0; }
-
-// The value of a name in `names`, or of an exact int.
-bool as_kind(PyObject* o, const char* const* names, int n, int32_t* v)
-{
-    if (PyUnicode_CheckExact(o)) {
-        for (int i = 0; i < n; ++i)
-            if (is(o, names[i])) {
-                *v = i;
-                return true;
-            }
-        return false;
-    }
-    return as_i32(o, v);
-}
 
 const char* const kMasks[] = {"none", "causal", "sliding_window", "prefix_lm",
                               "global_sliding_window", "share_question", "causal_blockwise"};
@@ -122,11 +49,6 @@ bool layout_array(const at::Tensor& t, const at::Tensor& q, int64_t nseq, int64_
     return true;
 }
 
-struct NoGil {
-    PyThreadState* state = PyEval_SaveThread();
-    ~NoGil() { PyEval_RestoreThread(state); }
-};
-
 enum Arg {
     kQ, kK, kV, kCausal, kWindow, kSlopes, kSoftcap, kScale, kCuQ, kCuK, kMaxQ, kMaxK, kOut, kLse,
     kReturnLse, kMask, kPrefix, kNumGlobal, kGlobalTokens, kSegments, kQueryStart, kRelPos, kNorm,
@@ -139,8 +61,7 @@ bool call(PyObject* const* a, at::Tensor* out, at::Tensor* lse, bool* with_lse, 
 {
     at::Tensor q, k, v;
     if (!plain(a[kQ], &q) || !plain(a[kK], &k) || !plain(a[kV], &v)) return false;
-    if (at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set())
-        return false;
+    if (modes()) return false;
     attn_variant_desc d = {};
     d.struct_size = sizeof(d);
     const auto dt = q.scalar_type();
@@ -301,23 +222,8 @@ PyObject* py_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
         bool with_lse = false;
         int status = ATTN_OK;
         if (!g_fwd_ws || !call(a, &out, &lse, &with_lse, &status)) Py_RETURN_NOTIMPLEMENTED;
-        if (status != ATTN_OK) {  // raises AttnError
-            PyObject* abi = PyImport_ImportModule("paper_2605_05023_amd._abi");
-            PyObject* none = abi ? PyObject_CallMethod(abi, "check", "i", status) : nullptr;
-            Py_XDECREF(abi);
-            return none;
-        }
-        PyObject* o = a[kOut] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[kOut]);
-        if (!o || !with_lse) return o;
-        PyObject* l = a[kLse] == Py_None ? THPVariable_Wrap(lse) : Py_NewRef(a[kLse]);
-        if (!l) {
-            Py_DECREF(o);
-            return nullptr;
-        }
-        PyObject* r = PyTuple_Pack(2, o, l);
-        Py_DECREF(o);
-        Py_DECREF(l);
-        return r;
+        if (status != ATTN_OK) return raise_status(status);
+        return outputs(a[kOut], out, a[kLse], lse, with_lse);
     } catch (const std::exception&) {
         // (out of memory, a device error): the Python path reports it
         PyErr_Clear();
@@ -339,6 +245,13 @@ PyMethodDef kMethods[] = {
     {"fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fwd)), METH_FASTCALL,
      "The attention forward, or NotImplemented where the Python path has to take the call."},
     {"bind", py_bind, METH_VARARGS, "Set the entry points of libattn.so."},
+    {"cache_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_plan)), METH_FASTCALL,
+     "cache_plan's outputs, or NotImplemented."},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_append)),
+     METH_FASTCALL, "None, or NotImplemented."},
+    {"cache_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_fwd)), METH_FASTCALL,
+     "cache_fwd's outputs, or NotImplemented."},
+    {"bind_cache", py_bind_cache, METH_VARARGS, "Set the entry points of the block cache."},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, kMethods, nullptr, nullptr, nullptr,
                        nullptr};

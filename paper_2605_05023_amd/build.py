@@ -69,7 +69,7 @@ def _build_binding() -> str:
            "-isystem", os.path.join(troot, "include"),
            "-isystem", os.path.join(troot, "include", "torch", "csrc", "api", "include"),
            "-isystem", "/opt/rocm/include", "-I", sysconfig.get_paths()["include"],
-           os.path.join(PKG, "binding", "fast.cpp"), "-L", os.path.join(troot, "lib"), "-lc10",
+           *(os.path.join(PKG, "binding", f) for f in ("fast.cpp", "fast_cache.cpp")), "-L", os.path.join(troot, "lib"), "-lc10",
            "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch", "-ltorch_python", "-o", out + ".tmp"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

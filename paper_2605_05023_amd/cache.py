@@ -29,6 +29,23 @@ _DTYPES = {torch.bfloat16: ATTN_BF16, torch.float32: ATTN_FP32}
 _FORMATS = {torch.float8_e4m3fn: ATTN_E4M3, torch.float8_e5m2: ATTN_E5M2}
 
 
+_native = None  # native argument marshalling (binding/fast_cache.cpp), bound to libattn.so
+
+
+def bind_native(fast, lib):
+    global _native
+    fast.bind_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.attn_cache_plan, lib.attn_cache_append, lib.attn_cache_fwd, lib.attn_cache_workspace_bytes)))
+    _native = fast
+
+
+def _marshal():
+    if _native is None:
+        from . import _load_native
+        _load_native()
+    return _native
+
+
 class KVCache(NamedTuple):
     """A pool of blocks: a stored value x of K stands for x * k_scale[block, head]."""
     k: torch.Tensor        # [blocks, kv heads, block size, head dim], float8_e4m3fn or float8_e5m2
@@ -137,6 +154,11 @@ def cache_plan(cached_lens, new_lens, block_tables, free_blocks, num_free, *, bl
     whose blocks are not there, or do not fit its row, is refused: its slots are -1
     and its seqlens_k stays its cached length.
     """
+    if not log:
+        res = (_native or _marshal()).cache_plan(cached_lens, new_lens, block_tables, free_blocks, num_free,
+                                                 block_size, total_new)
+        if res is not NotImplemented:
+            return CachePlan._make(res)
     _on_gpu(block_tables, "cache_plan")
     d, plan = make_plan_desc(cached_lens, new_lens, block_tables, free_blocks, num_free,
                              block_size=block_size, total_new=total_new, log=log)
@@ -182,6 +204,9 @@ def cache_append(cache: KVCache, k, v, slots, *, validate: bool = False, log: bo
     new values of a block need a larger one, its earlier values are stored anew.
     `validate` checks the order of the slots on the host first.
     """
+    if not (validate or log):
+        if (_native or _marshal()).cache_append(cache, k, v, slots) is not NotImplemented:
+            return
     _on_gpu(k, "cache_append")
     k, v = (t.contiguous() if _expanded(t) else t for t in (k, v))
     c, d = make_append_desc(cache, k, v, slots, validate=validate, log=log)
@@ -232,6 +257,14 @@ def cache_fwd(q, cache: KVCache, block_tables, seqlens_k, *, causal: bool = Fals
     the tables hold) is the longest key length, by which the keys are split over
     workgroups. Expanded q (an axis of stride 0) is copied first.
     """
+    if not (validate or log):
+        res = (_native or _marshal()).cache_fwd(
+            q, cache, block_tables, seqlens_k, causal, window, alibi_slopes, softcap, scale, cu_seqlens_q,
+            max_seqlen_q, max_seqlen_k, out, lse, return_lse)
+        if res is not NotImplemented:
+            return res
+    # options and arguments that the native marshalling does not take, and
+    # everything that is an error
     _on_gpu(q, "cache_fwd")
     if _expanded(q):
         q = q.contiguous()

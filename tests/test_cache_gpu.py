@@ -639,3 +639,66 @@ def test_poisoned_lds():
             _abi.check(which.attn_cache_plan(ctypes.byref(d)), which)
             got.append([*cache, *plan])
         assert all(bytes_equal(a, b) for a, b in zip(*got))
+
+
+# ---- native marshalling ---------------------------------------------------
+
+def test_native_marshalling_takes_the_calls():
+    """Ordinary calls go through binding/fast_cache.cpp and give the Python path's bits; the rest is
+    left to that path."""
+    native = attn._load_native()
+    c = attention_case(lens=[(1, 900), (2, 70)], alibi=True, seed=50)
+    cache = attn.KVCache(*(t.to(DEV) for t in c["pool"]))
+    q, table, lens, cu = c["q"].to(DEV), c["table"].to(DEV), i32([900, 70]), i32([0, 1, 3])
+    slopes = c["slopes"].to(DEV)
+    args = [q, cache, table, lens, True, (300, 0), slopes, 30, None, cu, 2, None, None, None, True]
+    got = native.cache_fwd(*args)
+    kw = dict(window=(300, 0), alibi_slopes=slopes, softcap=30, cu_seqlens_q=cu, max_seqlen_q=2)
+    want = attn.cache_fwd(q, cache, table, lens, log=True, **kw)  # log: the Python path
+    assert bytes_equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert bytes_equal(native.cache_fwd(*args[:-1], False), want[0])
+    out, lse = torch.empty_like(q), torch.empty_like(want[1])
+    res = native.cache_fwd(*args[:12], out, lse, True)
+    assert res[0] is out and res[1] is lse and bytes_equal(out, want[0])
+
+    x = torch.randn(3, 2, 128, device=DEV).bfloat16()
+    slots = torch.tensor([0, 64, 65], device=DEV)
+    caches = [attn.KVCache(*(t.clone() for t in cache)) for _ in range(2)]
+    assert native.cache_append(caches[0], x, x, slots) is None
+    attn.cache_append(caches[1], x, x, slots, log=True)
+    assert all(bytes_equal(a, b) for a, b in zip(*caches))
+    lens = [i32([900, 70]), i32([30, 5]), table.clone(), i32([3, 2, 1]), i32([3])]
+    a = native.cache_plan(*lens, 64, 40)
+    b = attn.cache_plan(*lens, block_size=64, total_new=40, log=True)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+    # not for it
+    assert native.cache_fwd(q.half(), *args[1:]) is NotImplemented
+    assert native.cache_fwd(*args[:2], table.long(), *args[3:]) is NotImplemented
+    assert native.cache_fwd(q, (cache.k, cache.v), *args[2:]) is NotImplemented
+    assert native.cache_append(caches[0], x.cpu(), x, slots) is NotImplemented
+    assert native.cache_plan(*lens, 48, 40) is NotImplemented
+    for bad in (dict(softcap=-1.0), dict(window=(-3, 0)), dict(max_seqlen_q=None)):
+        with pytest.raises((attn.AttnError, ValueError)):
+            attn.cache_fwd(q, cache, table, i32([900, 70]), **{**kw, **bad})
+    with pytest.raises(attn.AttnError):
+        attn.cache_plan(*lens, block_size=48, total_new=40)
+    with pytest.raises(ValueError):
+        attn.cache_append(caches[0], x.cpu(), x, slots)
+
+
+def test_a_failed_launch_is_raised_once():
+    native = attn._load_native()
+    lib, calls = attn.load(), []
+    failing = ctypes.CFUNCTYPE(ctypes.c_int, *[ctypes.c_void_p] * 4)(lambda *a: calls.append(1) or -7)
+    addr = [ctypes.cast(f, ctypes.c_void_p).value for f in
+            (lib.attn_cache_plan, failing, lib.attn_cache_fwd, lib.attn_cache_workspace_bytes)]
+    cache = attn.new_cache(2, 2, 16, 64)
+    x = torch.randn(1, 2, 64, device=DEV)
+    native.bind_cache(*addr)
+    try:
+        with pytest.raises(attn.AttnError) as e:
+            attn.cache_append(cache, x, x, torch.zeros(1, dtype=torch.int64, device=DEV))
+    finally:
+        attn._load_native()
+    assert e.value.status == -7 and len(calls) == 1
