@@ -244,6 +244,8 @@ int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdPar
     if (d.max_seqlen_k < 0 || d.table_width < 0 || d.stride_table < 0) return ATTN_ERR_BAD_SHAPE;
     p.stride_table = d.stride_table ? d.stride_table : d.table_width;
     if (d.batch > 1 && p.stride_table < d.table_width) return ATTN_ERR_BAD_SHAPE;
+    // keys are numbered with 31 bits, a chunk past the last included
+    if ((int64_t)d.table_width << p.pool.bshift > kInt32Max - 2 * kChunkKeys) return ATTN_ERR_UNSUPPORTED;
     const int64_t max_q = packed ? std::min<int64_t>(d.max_seqlen_q, d.total_q) : d.seqlen_q;
     const int64_t D = cache->head_dim, align = d.dtype == ATTN_BF16 ? 8 : 4;
     const int64_t rows = packed ? 0 : max_q;

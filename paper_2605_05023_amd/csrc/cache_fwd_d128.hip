@@ -11,7 +11,7 @@ hipError_t launch_cache_fwd_d128(const CacheFwdParams& p, const CacheFwdKind& ki
 
 int cache_tile_rows(const CacheFwdKind& kind)
 {
-    return kind.many_rows ? kWaves * 16 * kManyTiles : 16;
+    return !kind.many_rows ? 16 : kWaves * 16 * (kind.fp32 ? kManyTiles<float> : kManyTiles<__bf16>);
 }
 
 hipError_t launch_cache_fwd(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream)

@@ -17,9 +17,8 @@
 //    the scale of a block multiplies the score, that of V the probability,
 //    both in fp32. For fp32 calls q and P are split into three bf16 terms (24
 //    bits), each with products of its own into the same sums.
-// Few rows: the wavefronts of a workgroup take every fourth chunk of 64 keys and
-// are merged through LDS, and the keys are split over workgroups. Many rows:
-// they take row tiles of their own.
+// The wavefronts of a workgroup take every fourth chunk of 64 keys and are merged
+// through LDS, and the keys are split over workgroups (cache_many.h: many rows).
 #pragma once
 
 #include "cache_params.h"
@@ -95,7 +94,8 @@ __device__ __forceinline__ int split_size(const CacheFwdParams& p, int chunks)
 
 // Work item -> (kv group, row tile): the row tiles of a group follow one another
 // and, when the groups are a multiple of eight, on one XCD (ids are dealt
-// round-robin over the 8 XCDs), so that they meet in its L2.
+// round-robin over the 8 XCDs), so that they meet in its L2. The last ones, which
+// see the most keys under a causal mask, come first.
 __device__ __forceinline__ void work_item(const CacheFwdParams& p, uint32_t id, uint32_t* g, uint32_t* rt)
 {
     const uint32_t groups = (uint32_t)(p.batch * p.pool.hkv), nrt = (uint32_t)p.row_tiles;
@@ -107,6 +107,7 @@ __device__ __forceinline__ void work_item(const CacheFwdParams& p, uint32_t id, 
         *rt = id % nrt;
         *g = id / nrt;
     }
+    *rt = nrt - 1 - *rt;
 }
 
 template <bool E5M2, bool HI>
@@ -124,16 +125,56 @@ __device__ __forceinline__ bf16x8 to_bf16x8(uint32_t a, uint32_t b)
     return bf16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
 }
 
-// Sum and maximum over the lanes that share a row (lane mod 16).
+// Maximum and sum over the lanes that share a row (lane mod 16), without LDS:
+// each swap leaves the two halves (of 16, then 32 lanes) side by side.
+template <class F>
+__device__ __forceinline__ float over_row(float x, F f)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    const uint32_t c = __builtin_bit_cast(
+        uint32_t, f(__builtin_bit_cast(float, (uint32_t)p[0]), __builtin_bit_cast(float, (uint32_t)p[1])));
+    const auto q = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return f(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
 __device__ __forceinline__ float row_max(float x)
 {
-    x = __builtin_fmaxf(x, __shfl_xor(x, 16));
-    return __builtin_fmaxf(x, __shfl_xor(x, 32));
+    return over_row(x, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
 __device__ __forceinline__ float row_sum(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    return over_row(x, [](float a, float b) { return a + b; });
+}
+
+// Eight elements of q as NS bf16 terms.
+template <class T, int NS>
+__device__ __forceinline__ void load_q(const T* s, bf16x8 (&q)[NS])
+{
+    if constexpr (NS == 1) {
+        q[0] = *reinterpret_cast<const bf16x8*>(s);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = s[e];
+            const __bf16 a = (__bf16)x, b = (__bf16)(x - (float)a);
+            q[0][e] = a;
+            q[1][e] = b;
+            q[2][e] = (__bf16)(x - (float)a - (float)b);
+        }
+    }
+}
+
+// w as NS bf16 terms, element j of each.
+template <int NS>
+__device__ __forceinline__ void split_p(float w, bf16x8 (&p)[NS], int j)
+{
+    const __bf16 a = (__bf16)w;
+    p[0][j] = a;
+    if constexpr (NS == 3) {
+        const __bf16 b = (__bf16)(w - (float)a);
+        p[1][j] = b;
+        p[2][j] = (__bf16)(w - (float)a - (float)b);
+    }
 }
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
@@ -194,7 +235,7 @@ struct Writer {
 
 // T: element of q and out. MODS: soft-cap or ALiBi (one instantiation for both:
 // the vector work beside them is the conversion of K and V).
-template <int D, class T, bool E5M2, int MT, bool MODS, bool MANY>
+template <int D, class T, bool E5M2, int MT, bool MODS>
 __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
 {
     constexpr int NS = sizeof(T) == 2 ? 1 : 3;  // bf16 terms of q and P
@@ -219,19 +260,13 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
         split ? (((int64_t)group * p.row_tiles + rt) * p.splits + sp) * p.tile_rows : (int64_t)-1;
     const Writer<D, T> write{p, t, part};
 
-    const int fw = t.f0 + (MANY ? wave * WR : 0);  // the wavefront's first row
-    if (MANY && fw >= t.nflat) return;             // (no barrier under MANY)
-    // keys that any, and that every row of the wavefront sees
+    // keys that any, and that every row sees
     int64_t lo_any, hi_any, lo_all, hi_all;
     {
-        const int q0 = (int)fast_div((uint32_t)fw, p.div_group);
-        const int q1 = (int)fast_div((uint32_t)min(fw + WR, t.nflat) - 1u, p.div_group);
+        const int q0 = (int)fast_div((uint32_t)t.f0, p.div_group);
+        const int q1 = (int)fast_div((uint32_t)min(t.f0 + WR, t.nflat) - 1u, p.div_group);
         row_keys(p, t, q0, &lo_any, &hi_all);
         row_keys(p, t, q1, &lo_all, &hi_any);
-        if (MANY) {
-            c0 = max(c0, (int)(lo_any / kChunk));
-            c1 = hi_any > lo_any ? min(c1, (int)((hi_any + kChunk - 1) / kChunk)) : c0;
-        }
     }
 
     // q: lane holds dims 64 h + 16 g + 8 e .. + 7 of its row for product 2 h + e
@@ -241,7 +276,7 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
     float slope[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int f = min(fw + 16 * m + r, t.nflat - 1);
+        const int f = min(t.f0 + 16 * m + r, t.nflat - 1);
         const int qi = (int)fast_div((uint32_t)f, p.div_group);
         const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
         row_keys(p, t, qi, &jlo[m], &jhi[m]);
@@ -251,19 +286,7 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
                        (p.cu_q ? 0 : t.b * p.sq_b) + 16 * g;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const T* s = src + 64 * (k / 2) + 8 * (k % 2);
-            if constexpr (NS == 1) {
-                qf[m][k][0] = *reinterpret_cast<const bf16x8*>(s);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = s[e];
-                    const __bf16 a = (__bf16)x, b = (__bf16)(x - (float)a);
-                    qf[m][k][0][e] = a;
-                    qf[m][k][1][e] = b;
-                    qf[m][k][2][e] = (__bf16)(x - (float)a - (float)b);
-                }
-            }
+            load_q<T, NS>(src + 64 * (k / 2) + 8 * (k % 2), qf[m][k]);
         }
     }
 
@@ -286,7 +309,7 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
         return (uint32_t)page < (uint32_t)p.pool.num_blocks ? page : -1;
     };
 
-    for (int c = c0 + (MANY ? 0 : wave); c < c1; c += MANY ? 1 : kWaves) {
+    for (int c = c0 + wave; c < c1; c += kWaves) {
         const int64_t base = (int64_t)c * kChunk;
         const int64_t key_k = base + 16 * (r >> 2), key_v = base + 16 * g;
         const int page_k = page_of(key_k), page_v = page_of(key_v);
@@ -368,14 +391,7 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
             for (int j = 0; j < 16; ++j) {
                 const float e = __builtin_amdgcn_exp2f(x[j] - ref);
                 add += e;
-                const float w = e * vs;
-                const __bf16 a = (__bf16)w;
-                pf[m][j / 8][0][j % 8] = a;
-                if constexpr (NS == 3) {
-                    const __bf16 b = (__bf16)(w - (float)a);
-                    pf[m][j / 8][1][j % 8] = b;
-                    pf[m][j / 8][2][j % 8] = (__bf16)(w - (float)a - (float)b);
-                }
+                split_p<NS>(e * vs, pf[m][j / 8], j % 8);
             }
             sum[m] = __builtin_fmaf(sum[m], keep, add);
 #pragma unroll
@@ -395,59 +411,47 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
 
 #pragma unroll
     for (int m = 0; m < MT; ++m) sum[m] = row_sum(sum[m]);
-    if constexpr (MANY) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int f = fw + 16 * m + r;
-            if (f >= t.nflat) continue;
-            const float inv = write.factor(sum[m]);
-            if (g == 0) write.scalars(f, f - t.f0, mx[m], sum[m]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) write.out(f, f - t.f0, 16 * d + 4 * g, acc[m][d] * inv);
-        }
-    } else {
-        // merge the wavefronts: every row's O, maximum and sum through LDS (rows of
-        // D + 4 floats: the lanes of a quarter wave write 16 rows to other banks)
-        constexpr int LD = D + 4;
-        __shared__ __attribute__((aligned(16))) float lo_[kWaves][WR * LD];
-        __shared__ float lml[kWaves][WR][2];
-        if constexpr (kLdsPoison) {
-            for (int i = threadIdx.x; i < kWaves * WR * LD; i += NT)
-                (&lo_[0][0])[i] = __builtin_bit_cast(float, ~0u);
-            for (int i = threadIdx.x; i < kWaves * WR * 2; i += NT)
-                (&lml[0][0][0])[i] = __builtin_bit_cast(float, ~0u);
-            __syncthreads();
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (g == 0) {
-                lml[wave][16 * m + r][0] = mx[m];
-                lml[wave][16 * m + r][1] = sum[m];
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-                *reinterpret_cast<f32x4*>(&lo_[wave][(16 * m + r) * LD + 16 * d + 4 * g]) = acc[m][d];
-        }
+    // merge the wavefronts: every row's O, maximum and sum through LDS (rows of
+    // D + 4 floats: the lanes of a quarter wave write 16 rows to other banks)
+    constexpr int LD = D + 4;
+    __shared__ __attribute__((aligned(16))) float lo_[kWaves][WR * LD];
+    __shared__ float lml[kWaves][WR][2];
+    if constexpr (kLdsPoison) {
+        for (int i = threadIdx.x; i < kWaves * WR * LD; i += NT)
+            (&lo_[0][0])[i] = __builtin_bit_cast(float, ~0u);
+        for (int i = threadIdx.x; i < kWaves * WR * 2; i += NT)
+            (&lml[0][0][0])[i] = __builtin_bit_cast(float, ~0u);
         __syncthreads();
-        constexpr int COLS = D / 4;
-        for (int i = threadIdx.x; i < WR * COLS; i += NT) {
-            const int row = i / COLS, col = 4 * (i % COLS), f = t.f0 + row;
-            if (f >= t.nflat) break;
-            float top = -__builtin_inff(), l = 0.0f;
+    }
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = __builtin_fmaxf(top, lml[w][row][0]);
-            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                // (no key seen by any: weight 1 of nothing)
-                const float mw = lml[w][row][0];
-                const float k = mw == top ? 1.0f : __builtin_amdgcn_exp2f(mw - top);
-                l = __builtin_fmaf(lml[w][row][1], k, l);
-                o += *reinterpret_cast<const f32x4*>(&lo_[w][row * LD + col]) * k;
-            }
-            if (col == 0) write.scalars(f, row, top, l);
-            write.out(f, row, col, o * write.factor(l));
+    for (int m = 0; m < MT; ++m) {
+        if (g == 0) {
+            lml[wave][16 * m + r][0] = mx[m];
+            lml[wave][16 * m + r][1] = sum[m];
         }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<f32x4*>(&lo_[wave][(16 * m + r) * LD + 16 * d + 4 * g]) = acc[m][d];
+    }
+    __syncthreads();
+    constexpr int COLS = D / 4;
+    for (int i = threadIdx.x; i < WR * COLS; i += NT) {
+        const int row = i / COLS, col = 4 * (i % COLS), f = t.f0 + row;
+        if (f >= t.nflat) break;
+        float top = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = __builtin_fmaxf(top, lml[w][row][0]);
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            // (no key seen by any: weight 1 of nothing)
+            const float mw = lml[w][row][0];
+            const float k = mw == top ? 1.0f : __builtin_amdgcn_exp2f(mw - top);
+            l = __builtin_fmaf(lml[w][row][1], k, l);
+            o += *reinterpret_cast<const f32x4*>(&lo_[w][row * LD + col]) * k;
+        }
+        if (col == 0) write.scalars(f, row, top, l);
+        write.out(f, row, col, o * write.factor(l));
     }
 }
 

@@ -2,22 +2,24 @@
 #pragma once
 
 #include "cache_kernel.h"
+#include "cache_many.h"
 
 namespace attn {
 namespace {
 
-// Row tiles per wavefront: one for few rows (a decode step fills no more), two
-// for many, which halves the reads and conversions of K and V a row.
-constexpr int kManyTiles = 2;
+// 16-row tiles per wavefront of cache_many_kernel: the most that leave two
+// wavefronts a SIMD their registers (the three terms of fp32 q take 3/4 of one's).
+template <class T>
+constexpr int kManyTiles = sizeof(T) == 2 ? 2 : 1;
 
 template <int D, class T, bool E5M2, bool MODS>
 hipError_t launch_rows(const CacheFwdParams& p, bool many, hipStream_t stream)
 {
     const dim3 grid((unsigned)(p.batch * p.pool.hkv) * (unsigned)p.row_tiles, (unsigned)p.splits);
     if (many)
-        hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, kManyTiles, MODS, true>), grid, dim3(NT), 0, stream, p);
+        hipLaunchKernelGGL((cache_many_kernel<D, T, E5M2, kManyTiles<T>, MODS>), grid, dim3(NT), 0, stream, p);
     else
-        hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, 1, MODS, false>), grid, dim3(NT), 0, stream, p);
+        hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, 1, MODS>), grid, dim3(NT), 0, stream, p);
     return hipGetLastError();
 }
 

@@ -402,6 +402,21 @@ def test_freed_blocks_behind_a_window():
     check_case(c, validate=True)
 
 
+@pytest.mark.parametrize("n", [1, 40])
+def test_scales_of_zero_and_far_apart(n):
+    """A block whose scale is 0 holds zeros; neighbours may differ by many powers of two."""
+    for dt in ("bf16", "fp32"):
+        c = attention_case(dt=dt, bs=16, lens=[(n, 300), (n, 90)], hq=4, seed=21)
+        k, v, ks, vs = c["pool"]
+        for i, f in ((1, 0.0), (3, 2.0 ** -20), (7, 8.0)):
+            ks[c["table"][0, i]] *= f
+        for i, f in ((2, 0.0), (4, 2.0 ** -30), (9, 2.0 ** 20), (11, 0.0)):
+            vs[c["table"][0, i]] *= f
+        ks[c["table"][1, 0]] = 0.0
+        check_case(c)
+        check_case(dict(c, opt=dict(c["opt"], softcap=20.0)))
+
+
 def test_validate_refuses():
     def call(c, **kw):
         with pytest.raises(attn.AttnError):
