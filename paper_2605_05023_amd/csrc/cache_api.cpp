@@ -274,21 +274,24 @@ int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdPar
                                                      : -1;
     const double log2e = 1.4426950408889634;
     p.scale_u = (float)(d.scale * log2e);
+    p.softcap = d.softcap;
     p.cap_pre = d.softcap > 0.0f ? d.scale / d.softcap : 0.0f;
+    p.cap_pre2 = p.cap_pre * (float)(2.0 * log2e);
     p.cap_post = (float)(d.softcap * log2e);
     const int group = d.num_q_heads / cache->num_kv_heads;
     p.div_group = make_fastdiv((uint32_t)group);
     p.div_hkv = make_fastdiv((uint32_t)cache->num_kv_heads);
     s->max_q = d.batch == 0 ? 0 : max_q;
-    s->kind = {cache->head_dim, cache->cache_dtype == ATTN_E5M2, d.dtype == ATTN_FP32, false};
+    s->kind = {cache->head_dim, cache->cache_dtype == ATTN_E5M2, d.dtype == ATTN_FP32, false, 4, 1};
     // flat rows and workgroups are numbered with 31 bits
     const int64_t most = packed ? d.total_q : max_q;
     if (most * group > kInt32Max || (int64_t)d.batch * d.num_q_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
-    // Flat rows of a request at most: few of them share 16-row tiles whose keys are
-    // split over wavefronts, many take 128-row tiles.
+    // Flat rows of a request at most: up to 64 share tiles of 16 or 32 rows whose
+    // keys are split over wavefronts, more take tiles of 128 (fp32: 64).
     const int64_t flat = s->max_q * group;
     s->kind.many_rows = flat > 64;
-    p.tile_rows = attn::cache_tile_rows(s->kind);
+    s->kind.tiles = flat > 16 && !s->kind.fp32 ? 2 : 1;
+    p.tile_rows = 16 * s->kind.tiles * (s->kind.many_rows ? 4 : 1);
     const int64_t row_tiles = (flat + p.tile_rows - 1) / p.tile_rows;
     if (row_tiles * d.batch * cache->num_kv_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
     p.row_tiles = (int32_t)row_tiles;
@@ -428,7 +431,11 @@ extern "C" int attn_cache_fwd(const void* q, void* out, float* lse, const attn_c
                      p.slopes != nullptr, (double)d.softcap, s.kind.many_rows ? "many" : "few", p.tile_rows,
                      p.row_tiles, p.splits);
     hipStream_t stream = static_cast<hipStream_t>(d.stream);
-    hipError_t err = attn::launch_cache_fwd(p, s.kind, stream);
+    const bool d128 = s.kind.head_dim == 128;
+    hipError_t err = s.kind.e5m2 ? d128 ? attn::launch_cache_fwd_e5m2_d128(p, s.kind, stream)
+                                        : attn::launch_cache_fwd_e5m2_d64(p, s.kind, stream)
+                     : d128      ? attn::launch_cache_fwd_e4m3_d128(p, s.kind, stream)
+                                 : attn::launch_cache_fwd_e4m3_d64(p, s.kind, stream);
     if (err == hipSuccess && p.splits > 1) err = attn::launch_cache_combine(p, s.kind, stream);
     return launched(err, d.flags, "attn_cache_fwd");
 }

@@ -1,0 +1,11 @@
+// cache_fwd_e5m2_d64.hip -- attention to a block cache in e5m2, head dim 64.
+#include "cache_launch.h"
+
+namespace attn {
+
+hipError_t launch_cache_fwd_e5m2_d64(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream)
+{
+    return launch_type<64, true>(p, kind, stream);
+}
+
+}  // namespace attn

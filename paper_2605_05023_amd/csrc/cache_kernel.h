@@ -34,7 +34,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int NT = 256, kWaves = 4;
+constexpr int NT = 256, kWaves = 4;  // (the other kernels)
 constexpr int kChunk = 64;  // keys a wavefront takes at a time
 
 // A row tile of one kv group and the keys its rows see.
@@ -164,6 +164,19 @@ __device__ __forceinline__ void load_q(const T* s, bf16x8 (&q)[NS])
     }
 }
 
+// Wait for q here: a loop that may begin with its loads in flight waits for all
+// loads, those for the next chunk included, wherever it uses q.
+template <int MT, int KS, int NS>
+__device__ __forceinline__ void arrived(const bf16x8 (&q)[MT][KS][NS])
+{
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int n = 0; n < NS; ++n) asm volatile("" ::"v"(q[m][k][n]));
+}
+
 // w as NS bf16 terms, element j of each.
 template <int NS>
 __device__ __forceinline__ void split_p(float w, bf16x8 (&p)[NS], int j)
@@ -180,6 +193,104 @@ __device__ __forceinline__ void split_p(float w, bf16x8 (&p)[NS], int j)
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Score options, one instantiation each: ALiBi alone, the soft-cap in either
+// form (with ALiBi, whose slopes are then 0 where there are none).
+enum : int { kModsNone = 0, kModsAlibi = 1, kModsCapShort = 2, kModsCapExact = 3 };
+
+// What the softmax of one 16-row tile needs of the chunk: scores s of this lane's
+// sixteen keys (from `key` on) under the scales ks and vs of their block.
+struct ChunkScales {
+    float ks, lvs, ivs;  // K's scale; log2 and inverse of V's (of 1 where that is 0)
+    bool no_v;           // V's scale is 0
+    int key, page;       // first key; its block, -1: none
+    bool whole;          // every row of the wavefront sees all 64 keys, and no vs is 0
+};
+
+__device__ __forceinline__ ChunkScales chunk_scales(float ks, float vs, int key, int page, bool inside)
+{
+    ChunkScales c;  // (a page that is not there: scales of 0 in place of block 0's)
+    c.no_v = page < 0 || !(vs > 0.0f);
+    const float v = c.no_v ? 1.0f : vs;
+    c.ks = page < 0 ? 0.0f : ks;
+    c.lvs = __builtin_amdgcn_logf(v);
+    c.ivs = __builtin_amdgcn_rcpf(v);
+    c.key = key;
+    c.page = page;
+    c.whole = inside && __builtin_amdgcn_ballot_w64(c.no_v) == 0;
+    return c;
+}
+
+// One online-softmax step of a row tile: updates the running maximum, this
+// lane's share of the row sum and O, and gives P times V's scale as NS bf16
+// terms, the B operand of the P V products. P = 2^(score - maximum) and vs are
+// one exponential, of an FMA with the score's factors. The sum takes P without
+// vs. O and the sum are rescaled only where a maximum grows by more than 8 (P
+// stays below 2^8, whose bf16 has the same relative error).
+template <int NS, int DT, int MODS>
+__device__ __forceinline__ void softmax_step(const CacheFwdParams& p, const f32x4 (&s)[4],
+                                             const ChunkScales& c, int jlo, int jhi, int ip, float slope,
+                                             float& mx, float& sum, f32x4 (&acc)[DT], bf16x8 (&pf)[2][NS])
+{
+    float x[16];
+    float factor = c.ks * p.scale_u;  // x * factor is the score
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = s[j / 4][j % 4];
+    if constexpr (MODS != kModsNone) {
+        const float from = (float)(ip - c.key);
+        // the short form's error, 1e-4 at most (score_mods.h), is far below that of bf16
+        const float pre = c.ks * (MODS == kModsCapShort ? p.cap_pre2 : p.cap_pre);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if constexpr (MODS == kModsCapShort) x[j] = softcap_short_u(x[j], pre, p.cap_post);
+            else if constexpr (MODS == kModsCapExact) x[j] = softcap_u(x[j], pre, p.cap_post);
+            else x[j] *= factor;
+            x[j] = __builtin_fmaf(slope, __builtin_fabsf(from - (float)j), x[j]);
+        }
+        factor = 1.0f;
+    }
+    if (!c.whole) {
+        asm volatile("");  // a branch: most chunks are whole, and the selects are as long as the rest
+        const int lo = jlo - c.key, hi = c.page < 0 ? 0 : jhi - c.key;
+        // (a scale of 0: its scores are 0, not 0 * -inf)
+        const bool zero = factor == 0.0f;
+        factor = zero ? 1.0f : factor;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            x[j] = j >= lo && j < hi ? zero ? 0.0f : x[j] : -__builtin_inff();
+    }
+    float top[6];
+#pragma unroll
+    for (int j = 0; j < 5; ++j)
+        top[j] = __builtin_fmaxf(__builtin_fmaxf(x[3 * j], x[3 * j + 1]), x[3 * j + 2]);
+    top[5] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), top[2]);
+    top[5] = __builtin_fmaxf(__builtin_fmaxf(top[3], top[4]), __builtin_fmaxf(top[5], x[15]));
+    const float now = row_max(top[5] * factor);
+    if (__builtin_amdgcn_ballot_w64(now > mx + 8.0f)) {
+        const float to = __builtin_fmaxf(mx, now);
+        // (a row without a key so far: nothing to scale, and not 2^(inf - inf))
+        const float keep = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(mx - to);
+        mx = to;
+        sum *= keep;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] *= keep;
+    }
+    const float shift = c.lvs - (mx == -__builtin_inff() ? 0.0f : mx);
+    float add[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], factor, shift));
+        add[j % 4] += e;
+        split_p<NS>(e, pf[j / 8], j % 8);
+    }
+    sum = __builtin_fmaf((add[0] + add[1]) + (add[2] + add[3]), c.ivs, sum);
+    if (!c.whole && c.no_v) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int n = 0; n < NS; ++n) pf[k][n] = bf16x8{};
+    }
 }
 
 // The bytes of dword i of a lane's sixteen keys that lie in [lo, hi).
@@ -233,10 +344,9 @@ struct Writer {
     }
 };
 
-// T: element of q and out. MODS: soft-cap or ALiBi (one instantiation for both:
-// the vector work beside them is the conversion of K and V).
-template <int D, class T, bool E5M2, int MT, bool MODS>
-__global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
+// T: element of q and out.
+template <int D, class T, bool E5M2, int MT, int MODS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_fwd_kernel(CacheFwdParams p)
 {
     constexpr int NS = sizeof(T) == 2 ? 1 : 3;  // bf16 terms of q and P
     constexpr int WR = 16 * MT;                 // rows of a wavefront
@@ -261,27 +371,32 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
     const Writer<D, T> write{p, t, part};
 
     // keys that any, and that every row sees
-    int64_t lo_any, hi_any, lo_all, hi_all;
+    int lo_any, hi_any, lo_all, hi_all;
     {
-        const int q0 = (int)fast_div((uint32_t)t.f0, p.div_group);
-        const int q1 = (int)fast_div((uint32_t)min(t.f0 + WR, t.nflat) - 1u, p.div_group);
-        row_keys(p, t, q0, &lo_any, &hi_all);
-        row_keys(p, t, q1, &lo_all, &hi_any);
+        int64_t a, b, c, d;
+        row_keys(p, t, (int)fast_div((uint32_t)t.f0, p.div_group), &a, &d);
+        row_keys(p, t, (int)fast_div((uint32_t)min(t.f0 + WR, t.nflat) - 1u, p.div_group), &c, &b);
+        lo_any = (int)min(a, t.kend);
+        hi_any = (int)max(b, (int64_t)0);
+        lo_all = (int)min(c, t.kend);
+        hi_all = (int)max(d, (int64_t)0);
     }
 
     // q: lane holds dims 64 h + 16 g + 8 e .. + 7 of its row for product 2 h + e
     bf16x8 qf[MT][KS][NS];
-    int64_t jlo[MT], jhi[MT];
-    int64_t ip[MT];
+    int jlo[MT], jhi[MT], ip[MT];
     float slope[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int f = min(t.f0 + 16 * m + r, t.nflat - 1);
         const int qi = (int)fast_div((uint32_t)f, p.div_group);
         const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
-        row_keys(p, t, qi, &jlo[m], &jhi[m]);
-        ip[m] = qi + t.lk - t.lq;
-        slope[m] = MODS && p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
+        int64_t a, b;
+        row_keys(p, t, qi, &a, &b);
+        jlo[m] = (int)min(a, t.kend);
+        jhi[m] = (int)max(b, (int64_t)0);
+        ip[m] = (int)(qi + t.lk - t.lq);
+        slope[m] = MODS != kModsNone && p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
         const T* src = static_cast<const T*>(p.q) + (p.cu_q ? t.qrow0 + qi : qi) * p.sq_s + h * p.sq_h +
                        (p.cu_q ? 0 : t.b * p.sq_b) + 16 * g;
 #pragma unroll
@@ -302,29 +417,37 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
 
     const int bshift = p.pool.bshift, bs1 = (1 << bshift) - 1;
     const int32_t* table = p.table + t.b * p.stride_table;
-    // page of the 16 keys from key16 on; -1 where no row sees any or the entry is bad
-    auto page_of = [&](int64_t key16) __attribute__((always_inline)) -> int {
-        if (key16 >= hi_any || key16 + 16 <= lo_any) return -1;
-        const int page = table[key16 >> bshift];
-        return (uint32_t)page < (uint32_t)p.pool.num_blocks ? page : -1;
+    // The table entries of a chunk's keys are read one chunk ahead, without a
+    // branch (a column past the end is the last one); which of them count is
+    // decided when they are used: -1 where no row sees any of the 16 keys from
+    // key16 on, or the entry is none of a block.
+    int entry_k = -1, entry_v = -1;
+    auto fetch = [&](int c) __attribute__((always_inline)) {
+        entry_k = table[min((c * kChunk + 16 * (r >> 2)) >> bshift, p.width - 1)];
+        entry_v = table[min((c * kChunk + 16 * g) >> bshift, p.width - 1)];
     };
-
-    for (int c = c0 + wave; c < c1; c += kWaves) {
-        const int64_t base = (int64_t)c * kChunk;
-        const int64_t key_k = base + 16 * (r >> 2), key_v = base + 16 * g;
-        const int page_k = page_of(key_k), page_v = page_of(key_v);
+    auto page_of = [&](int key16, int entry) __attribute__((always_inline)) -> int {
+        return key16 < hi_any && key16 + 16 > lo_any && (uint32_t)entry < (uint32_t)p.pool.num_blocks ? entry
+                                                                                                      : -1;
+    };
+    if (c0 + wave < c1) fetch(c0 + wave);
+    arrived(qf);
+    for (int c = c0 + wave; c < c1; c += WAVES) {
+        const int base = c * kChunk, key_k = base + 16 * (r >> 2), key_v = base + 16 * g;
+        const int page_k = page_of(key_k, entry_k), page_v = page_of(key_v, entry_v);
+        fetch(c + WAVES);
         // (a page that is not there: block 0 is read and masked out)
         const uint8_t* kp = p.pool.k + (int64_t)max(page_k, 0) * p.pool.sk_b + t.hkv * p.pool.sk_h +
-                            (((int)key_k & bs1) + (r & 3)) * D + 16 * g;
+                            ((key_k & bs1) + (r & 3)) * D + 16 * g;
         const uint8_t* vp = p.pool.v + (int64_t)max(page_v, 0) * p.pool.sv_b + t.hkv * p.pool.sv_h +
-                            (r << bshift) + ((int)key_v & bs1);
+                            (r << bshift) + (key_v & bs1);
         u32x4 kw[4][HV], vw[DT];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int h = 0; h < HV; ++h) kw[u][h] = *reinterpret_cast<const u32x4*>(kp + 4 * u * D + 64 * h);
-        const float ks = page_v < 0 ? 0.0f : p.pool.k_scale[page_v * p.pool.sks_b + t.hkv];
-        const float vs = page_v < 0 ? 0.0f : p.pool.v_scale[page_v * p.pool.svs_b + t.hkv];
+        const float ks = p.pool.k_scale[max(page_v, 0) * p.pool.sks_b + t.hkv];
+        const float vs = p.pool.v_scale[max(page_v, 0) * p.pool.svs_b + t.hkv];
 #pragma unroll
         for (int d = 0; d < DT; ++d) vw[d] = *reinterpret_cast<const u32x4*>(vp + (d << (4 + bshift)));
 
@@ -343,13 +466,12 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
             }
         }
 
-        // whole: every row sees all 64 keys, in pages that are there
-        const bool whole = base >= lo_all && base + kChunk <= hi_all &&
-                           __builtin_amdgcn_ballot_w64(page_v < 0) == 0;
-        if (!whole) {
+        const ChunkScales cs =
+            chunk_scales(ks, vs, key_v, page_v, base >= lo_all && base + kChunk <= hi_all);
+        if (!cs.whole) {
             // bytes of V that no row sees weigh 0, whatever they hold
-            const int lo = (int)min(max(lo_any - key_v, (int64_t)0), (int64_t)16);
-            const int hi = page_v < 0 ? 0 : (int)min(max(hi_any - key_v, (int64_t)0), (int64_t)16);
+            const int lo = min(max(lo_any - key_v, 0), 16);
+            const int hi = page_v < 0 ? 0 : min(max(hi_any - key_v, 0), 16);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t keep = byte_mask(i, lo, hi);
@@ -360,43 +482,9 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
 
         bf16x8 pf[MT][2][NS];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            float x[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float dot = s[m][j / 4][j % 4] * ks;
-                if constexpr (MODS) {
-                    x[j] = p.cap_post != 0.0f ? softcap_u(dot, p.cap_pre, p.cap_post) : dot * p.scale_u;
-                    x[j] = __builtin_fmaf(slope[m], __builtin_fabsf((float)(int)(ip[m] - key_v - j)), x[j]);
-                } else {
-                    x[j] = dot * p.scale_u;
-                }
-            }
-            if (!whole) {
-                const int lo = (int)min(max(jlo[m] - key_v, (int64_t)0), (int64_t)16);
-                const int hi = page_v < 0 ? 0 : (int)min(max(jhi[m] - key_v, (int64_t)0), (int64_t)16);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) x[j] = j >= lo && j < hi ? x[j] : -__builtin_inff();
-            }
-            float top = x[0];
-#pragma unroll
-            for (int j = 1; j < 16; ++j) top = __builtin_fmaxf(top, x[j]);
-            const float now = __builtin_fmaxf(mx[m], row_max(top));
-            // a row that has seen no key yet: exponents of 0 - inf, not inf - inf
-            const float ref = now == -__builtin_inff() ? 0.0f : now;
-            const float keep = __builtin_amdgcn_exp2f(mx[m] - ref);
-            mx[m] = now;
-            float add = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float e = __builtin_amdgcn_exp2f(x[j] - ref);
-                add += e;
-                split_p<NS>(e * vs, pf[m][j / 8], j % 8);
-            }
-            sum[m] = __builtin_fmaf(sum[m], keep, add);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[m][d] *= keep;
-        }
+        for (int m = 0; m < MT; ++m)
+            softmax_step<NS, DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m],
+                                       pf[m]);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -414,12 +502,12 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
     // merge the wavefronts: every row's O, maximum and sum through LDS (rows of
     // D + 4 floats: the lanes of a quarter wave write 16 rows to other banks)
     constexpr int LD = D + 4;
-    __shared__ __attribute__((aligned(16))) float lo_[kWaves][WR * LD];
-    __shared__ float lml[kWaves][WR][2];
+    __shared__ __attribute__((aligned(16))) float lo_[WAVES][WR * LD];
+    __shared__ float lml[WAVES][WR][2];
     if constexpr (kLdsPoison) {
-        for (int i = threadIdx.x; i < kWaves * WR * LD; i += NT)
+        for (int i = threadIdx.x; i < WAVES * WR * LD; i += 64 * WAVES)
             (&lo_[0][0])[i] = __builtin_bit_cast(float, ~0u);
-        for (int i = threadIdx.x; i < kWaves * WR * 2; i += NT)
+        for (int i = threadIdx.x; i < WAVES * WR * 2; i += 64 * WAVES)
             (&lml[0][0][0])[i] = __builtin_bit_cast(float, ~0u);
         __syncthreads();
     }
@@ -435,15 +523,15 @@ __global__ __launch_bounds__(NT, 2) void cache_fwd_kernel(CacheFwdParams p)
     }
     __syncthreads();
     constexpr int COLS = D / 4;
-    for (int i = threadIdx.x; i < WR * COLS; i += NT) {
+    for (int i = threadIdx.x; i < WR * COLS; i += 64 * WAVES) {
         const int row = i / COLS, col = 4 * (i % COLS), f = t.f0 + row;
         if (f >= t.nflat) break;
         float top = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = __builtin_fmaxf(top, lml[w][row][0]);
+        for (int w = 0; w < WAVES; ++w) top = __builtin_fmaxf(top, lml[w][row][0]);
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             // (no key seen by any: weight 1 of nothing)
             const float mw = lml[w][row][0];
             const float k = mw == top ? 1.0f : __builtin_amdgcn_exp2f(mw - top);

@@ -14,10 +14,7 @@
 // under an XOR of the piece's index with bits of the row, such that the 16 rows
 // that a quarter of a wavefront reads (and the rows it writes) lie in all 64
 // banks.
-// Per score: half a v_max3, an FMA (the scale of the block, the running maximum
-// and log2 of V's scale in one), an exponential, an add and half a conversion.
-// O and the sums are rescaled only where a running maximum grows by more than 8
-// (P stays below 2^8, whose bf16 has the same relative error).
+// Per score: half a v_max3, an FMA, an exponential, an add and half a conversion.
 #pragma once
 
 #include "cache_kernel.h"
@@ -38,7 +35,7 @@ __device__ __forceinline__ int v_piece(int row, int c)
     return row * 128 + ((c ^ (row >> 1 & 7)) << 4);
 }
 
-template <int D, class T, bool E5M2, int MT, bool MODS>
+template <int D, class T, bool E5M2, int MT, int MODS>
 __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
 {
     constexpr int NS = sizeof(T) == 2 ? 1 : 3;
@@ -103,7 +100,7 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
         jlo[m] = (int)min(a, t.kend);
         jhi[m] = (int)max(b, (int64_t)0);
         ip[m] = (int)(qi + t.lk - t.lq);
-        slope[m] = MODS && p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
+        slope[m] = MODS != kModsNone && p.slopes ? -p.slopes[h] * kLog2e : 0.0f;
         const T* src = static_cast<const T*>(p.q) + (p.cu_q ? t.qrow0 + qi : qi) * p.sq_s + h * p.sq_h +
                        (p.cu_q ? 0 : t.b * p.sq_b) + 8 * g;
 #pragma unroll
@@ -120,8 +117,9 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
         for (int d = 0; d < DT; ++d) acc[m][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // Loads of one chunk: pages of its four groups of 16 keys (one table entry
-    // where blocks are larger), then this thread's pieces.
+    // Loads of one chunk. The table entries of its four groups of 16 keys (one where
+    // blocks are larger) are read one chunk earlier, a lane the entry of group
+    // lane % 4, without a branch (a column past the end is the last one).
     const int bshift = p.pool.bshift, bs1 = (1 << bshift) - 1;
     const int32_t* table = p.table + t.b * p.stride_table;
     const uint8_t* kbase = p.pool.k + t.hkv * p.pool.sk_h;
@@ -129,30 +127,39 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
     struct Staged {
         u32x4 k[PIECES], v[PIECES];
         float ks, vs;
-        int page_v;    // of this thread's pieces of V
+        int page_v;    // of this thread's pieces of V; -1: none
         int page_s;    // of the keys whose scores this lane holds
     };
-    auto page_of = [&](int key16) __attribute__((always_inline)) -> int {
-        if (key16 >= hi_wg || key16 + 16 <= lo_wg) return -1;
-        const int page = table[key16 >> bshift];
-        return (uint32_t)page < (uint32_t)p.pool.num_blocks ? page : -1;
+    int entry = -1;
+    auto fetch = [&](int c) __attribute__((always_inline)) {
+        entry = table[min((c * kChunk + 16 * (lane & 3)) >> bshift, p.width - 1)];
     };
     auto load = [&](int c, Staged& s) __attribute__((always_inline)) {
-        const int base = c * kChunk;
-        s.page_s = page_of(base + 16 * g);
-        s.page_v = page_of(base + 16 * (tid & 3));
+        // -1 where no row of the workgroup sees any of the 16 keys, or the entry is
+        // none of a block
+        const int base = c * kChunk, mine = base + 16 * (lane & 3);
+        const int page = mine < hi_wg && mine + 16 > lo_wg && (uint32_t)entry < (uint32_t)p.pool.num_blocks
+                             ? entry
+                             : -1;
+        const int pages[4] = {__builtin_amdgcn_readlane(page, 0), __builtin_amdgcn_readlane(page, 1),
+                              __builtin_amdgcn_readlane(page, 2), __builtin_amdgcn_readlane(page, 3)};
+        fetch(c + 1);
+        s.page_v = page;
+        s.page_s = g & 2 ? g & 1 ? pages[3] : pages[2] : g & 1 ? pages[1] : pages[0];
+        s.ks = p.pool.k_scale[max(s.page_s, 0) * p.pool.sks_b + t.hkv];
+        s.vs = p.pool.v_scale[max(s.page_s, 0) * p.pool.svs_b + t.hkv];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
+            // (a wavefront's pieces of K lie in one group)
             const int piece = tid + NT * i, row = piece / (D / 16), col = piece % (D / 16);
-            const int page = page_of(base + (row & ~15));
-            s.k[i] = *reinterpret_cast<const u32x4*>(kbase + (int64_t)max(page, 0) * p.pool.sk_b +
+            const int kg = D == 128 ? 2 * i + (wave >> 1) : wave;
+            const int page_k = kg & 2 ? kg & 1 ? pages[3] : pages[2] : kg & 1 ? pages[1] : pages[0];
+            s.k[i] = *reinterpret_cast<const u32x4*>(kbase + (int64_t)max(page_k, 0) * p.pool.sk_b +
                                                      ((base + row) & bs1) * D + 16 * col);
             const int d = piece >> 2;
-            s.v[i] = *reinterpret_cast<const u32x4*>(vbase + (int64_t)max(s.page_v, 0) * p.pool.sv_b +
-                                                     (d << bshift) + ((base + 16 * (tid & 3)) & bs1));
+            s.v[i] = *reinterpret_cast<const u32x4*>(vbase + (int64_t)max(page, 0) * p.pool.sv_b +
+                                                     (d << bshift) + (mine & bs1));
         }
-        s.ks = s.page_s < 0 ? 0.0f : p.pool.k_scale[s.page_s * p.pool.sks_b + t.hkv];
-        s.vs = s.page_s < 0 ? 0.0f : p.pool.v_scale[s.page_s * p.pool.svs_b + t.hkv];
     };
     auto store = [&](int c, const Staged& s, char* k, char* v) __attribute__((always_inline)) {
         const int base = c * kChunk;
@@ -180,10 +187,12 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
 
     Staged next;
     if (c0 < c1) {
+        fetch(c0);
         load(c0, next);
         store(c0, next, lds[0][0], lds[0][1]);
     }
     __syncthreads();
+    arrived(qf);
     for (int c = c0; c < c1; ++c) {
         const int base = c * kChunk, key = base + 16 * g;
         const float ks = next.ks, vs = next.vs;
@@ -209,68 +218,13 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
                 }
             }
 
-            // whole: every row sees all 64 keys, in pages that are there, and no V
-            // scale is 0 (its logarithm below)
-            const bool whole = base >= lo_all && base + kChunk <= hi_all &&
-                               __builtin_amdgcn_ballot_w64(page < 0 || !(vs > 0.0f)) == 0;
-            const float vs1 = vs > 0.0f ? vs : 1.0f, lvs = __builtin_log2f(vs1), ivs = 1.0f / vs1;
+            const ChunkScales cs =
+                chunk_scales(ks, vs, key, page, base >= lo_all && base + kChunk <= hi_all);
             bf16x8 pf[MT][2][NS];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                float x[16];
-                float factor = ks * p.scale_u;  // x * factor is the score
-#pragma unroll
-                for (int j = 0; j < 16; ++j) x[j] = s[m][j / 4][j % 4];
-                if constexpr (MODS) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float dot = x[j] * ks;
-                        x[j] = p.cap_post != 0.0f ? softcap_u(dot, p.cap_pre, p.cap_post) : dot * p.scale_u;
-                        x[j] = __builtin_fmaf(slope[m], __builtin_fabsf((float)(ip[m] - key - j)), x[j]);
-                    }
-                    factor = 1.0f;
-                }
-                if (!whole) {
-                    const int lo = jlo[m] - key, hi = page < 0 ? 0 : jhi[m] - key;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = j >= lo && j < hi ? x[j] : -__builtin_inff();
-                }
-                float top = x[0];
-#pragma unroll
-                for (int j = 1; j < 16; ++j) top = __builtin_fmaxf(top, x[j]);
-                // (a scale of 0: its scores are 0, not 0 * -inf)
-                if (!whole && factor == 0.0f) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = x[j] == -__builtin_inff() ? x[j] : 0.0f;
-                    top = top == -__builtin_inff() ? top : 0.0f;
-                    factor = 1.0f;
-                }
-                const float now = row_max(top * factor);
-                if (__builtin_amdgcn_ballot_w64(now > mx[m] + 8.0f)) {
-                    const float to = __builtin_fmaxf(mx[m], now);
-                    const float keep = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(mx[m] - to);
-                    mx[m] = to;
-                    sum[m] *= keep;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) acc[m][d] *= keep;
-                }
-                // P times V's scale; a row that has seen no key yet: 2^(-inf - 0)
-                const float shift = lvs - (mx[m] == -__builtin_inff() ? 0.0f : mx[m]);
-                float add = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], factor, shift));
-                    add += e;
-                    split_p<NS>(e, pf[m][j / 8], j % 8);
-                }
-                sum[m] = __builtin_fmaf(add, ivs, sum[m]);
-                if (!whole && !(vs > 0.0f)) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int n = 0; n < NS; ++n) pf[m][k][n] = bf16x8{};
-                }
-            }
+            for (int m = 0; m < MT; ++m)
+                softmax_step<NS, DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m],
+                                           acc[m], pf[m]);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll

@@ -60,7 +60,8 @@ struct CacheFwdParams {
     int32_t batch, hq, seqlen_q, width;
     int32_t wl, wr;          // window bounds, -1 = unbounded (causal: wr = 0)
     float scale_u;           // scale * log2(e)
-    float cap_pre, cap_post; // soft-cap C: scale / C and C log2(e); cap_post 0 = off
+    float softcap;           // C, 0 = off
+    float cap_pre, cap_pre2, cap_post;  // scale / C, 2 log2(e) scale / C, C log2(e)
     FastDiv div_group;       // query heads of a kv head
     FastDiv div_hkv;
     // Flat row f of a kv group is query f / group of head f % group;
@@ -74,19 +75,22 @@ struct CacheFwdParams {
     float* ws_ml;
 };
 
-// Variants of the attention kernel.
+// Variants of the attention kernel. waves: wavefronts of a workgroup, 4 or (few
+// rows) 8; tiles: 16-row tiles of a wavefront.
 struct CacheFwdKind {
     int head_dim;
     bool e5m2, fp32, many_rows;
+    int waves, tiles;
 };
 
 hipError_t launch_cache_plan(const CachePlanParams& p, hipStream_t stream);
 hipError_t launch_cache_append(const CacheAppendParams& p, int head_dim, bool e5m2, bool fp32,
                                hipStream_t stream);
-int cache_tile_rows(const CacheFwdKind& kind);
-hipError_t launch_cache_fwd(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
-hipError_t launch_cache_fwd_d128(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
-hipError_t launch_cache_fwd_d64(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
+// one translation unit for each format and head dim
+hipError_t launch_cache_fwd_e4m3_d128(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
+hipError_t launch_cache_fwd_e4m3_d64(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
+hipError_t launch_cache_fwd_e5m2_d128(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
+hipError_t launch_cache_fwd_e5m2_d64(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
 hipError_t launch_cache_combine(const CacheFwdParams& p, const CacheFwdKind& kind, hipStream_t stream);
 
 }  // namespace attn
