@@ -35,6 +35,22 @@ __device__ __forceinline__ int v_piece(int row, int c)
     return row * 128 + ((c ^ (row >> 1 & 7)) << 4);
 }
 
+// Order of one set of products: four operand reads ahead, then one for every
+// operand used (`uses` products each). The compiler's own order reads an operand
+// one product before it is waited for: 4096 queries over 8192 keys 476 against
+// 453 us.
+template <int READS, int USES, int SET>
+__device__ __forceinline__ void issue_order()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, SET);
+#pragma unroll
+    for (int i = 0; i < READS - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, USES, SET);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, SET);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4 * USES, SET);
+}
+
 template <int D, class T, bool E5M2, int MT, int MODS>
 __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
 {
@@ -218,6 +234,7 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
                 }
             }
 
+            issue_order<4 * KS, MT * NS, 0>();
             const ChunkScales cs =
                 chunk_scales(ks, vs, key, page, base >= lo_all && base + kChunk <= hi_all);
             bf16x8 pf[MT][2][NS];
@@ -235,6 +252,7 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
 #pragma unroll
                         for (int n = NS - 1; n >= 0; --n) acc[m][d] = mfma(a, pf[m][k][n], acc[m][d]);
                 }
+            issue_order<2 * DT, MT * NS, 1>();
         }
         if (more) store(c + 1, next, lds[(c + 1 - c0) & 1][0], lds[(c + 1 - c0) & 1][1]);
         __syncthreads();

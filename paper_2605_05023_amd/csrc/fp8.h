@@ -31,7 +31,12 @@ struct Fp8 {
     // Four floats to bytes, to nearest even, limited to +-kMax; NaN stays NaN.
     static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d)
     {
-        a = limit(a), b = limit(b), c = limit(c), d = limit(d);
+        return round(limit(a), limit(b), limit(c), limit(d));
+    }
+
+    // The same of floats within +-kMax.
+    static __device__ __forceinline__ uint32_t round(float a, float b, float c, float d)
+    {
         if constexpr (E5M2) {
             const int lo = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false);
             return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(c, d, lo, true);
