@@ -395,7 +395,8 @@ int attn_cache_append(const void *k, const void *v, const attn_cache *cache,
  * instructions and fp32 sums, the scales applied in fp32 (fp32 q and P are split
  * into three bf16 terms, so nothing is lost).
  * The workspace is that of attn_fwd_ws: attn_cache_workspace_bytes says how much
- * the call can use, NULL or less computes it without splitting the keys.
+ * the call can use (a quarter of the bytes of q, out, K and V at most, or 256 MiB
+ * where that is more), NULL or less computes it without splitting the keys.
  */
 typedef struct attn_cache_fwd_desc {
     uint32_t struct_size;
@@ -422,6 +423,15 @@ typedef struct attn_cache_fwd_desc {
     int64_t stride_q_b, stride_q_h, stride_q_s;
     int64_t stride_o_b, stride_o_h, stride_o_s;
     void *stream;
+    /* Schedule overrides for tuning and tests (0 = the library's choice); they
+       change the order of the sums, nothing else.                            */
+    int32_t sched_kernel;        /* 1: few rows, 2: many rows (a workgroup's row
+                                    tile is one or sched_waves wavefronts')       */
+    int32_t sched_waves;         /* wavefronts of a workgroup, 4 or 8 (many rows
+                                    at head_dim 64: 4)                            */
+    int32_t sched_tiles;         /* 16-row tiles of a wavefront, 1 or 2 (fp32: 1;
+                                    many rows of bf16: 2)                         */
+    int32_t sched_splits;        /* key splits, 1 .. 64 (1 without a workspace)   */
 } attn_cache_fwd_desc;
 
 int64_t attn_cache_workspace_bytes(const attn_cache *cache, const attn_cache_fwd_desc *desc);

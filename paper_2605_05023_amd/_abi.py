@@ -119,6 +119,8 @@ class AttnCacheFwdDesc(_Sized):
         ("stride_q_b", ctypes.c_int64), ("stride_q_h", ctypes.c_int64), ("stride_q_s", ctypes.c_int64),
         ("stride_o_b", ctypes.c_int64), ("stride_o_h", ctypes.c_int64), ("stride_o_s", ctypes.c_int64),
         ("stream", ctypes.c_void_p),
+        ("sched_kernel", ctypes.c_int32), ("sched_waves", ctypes.c_int32),
+        ("sched_tiles", ctypes.c_int32), ("sched_splits", ctypes.c_int32),
     ]
 
 

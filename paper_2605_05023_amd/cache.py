@@ -246,7 +246,7 @@ def _lse_shape(q, packed):
 def cache_fwd(q, cache: KVCache, block_tables, seqlens_k, *, causal: bool = False, window=None,
               alibi_slopes=None, softcap: float = 0.0, scale: Optional[float] = None, cu_seqlens_q=None,
               max_seqlen_q=None, max_seqlen_k=None, out=None, lse=None, return_lse: bool = True,
-              validate: bool = False, log: bool = False):
+              validate: bool = False, log: bool = False, schedule=None):
     """Softmax attention of new queries to the cached keys of their requests.
 
     q: [batch, heads, queries, head dim], or packed [tokens, heads, head dim] with
@@ -255,9 +255,11 @@ def cache_fwd(q, cache: KVCache, block_tables, seqlens_k, *, causal: bool = Fals
     position seqlens_k - n + i. block_tables: int32 [batch, width].
     Masks, score options and outputs are those of `fwd`; max_seqlen_k (default: what
     the tables hold) is the longest key length, by which the keys are split over
-    workgroups. Expanded q (an axis of stride 0) is copied first.
+    workgroups. Expanded q (an axis of stride 0) is copied first. `schedule`, a dict
+    of the descriptor's sched_* overrides ("kernel", "waves", "tiles", "splits"), is
+    for tuning and tests.
     """
-    if not (validate or log):
+    if not (validate or log or schedule):
         res = (_native or _marshal()).cache_fwd(
             q, cache, block_tables, seqlens_k, causal, window, alibi_slopes, softcap, scale, cu_seqlens_q,
             max_seqlen_q, max_seqlen_k, out, lse, return_lse)
@@ -276,7 +278,7 @@ def cache_fwd(q, cache: KVCache, block_tables, seqlens_k, *, causal: bool = Fals
     c, d = make_fwd_desc(q, cache, block_tables, seqlens_k, out, lse, causal=causal, window=window,
                          alibi_slopes=alibi_slopes, softcap=softcap, scale=scale,
                          cu_seqlens_q=cu_seqlens_q, max_seqlen_q=max_seqlen_q,
-                         max_seqlen_k=max_seqlen_k, validate=validate, log=log)
+                         max_seqlen_k=max_seqlen_k, validate=validate, log=log, schedule=schedule)
     lib = load()
     nbytes = lib.attn_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(d))
     ws = None
@@ -294,7 +296,7 @@ def cache_fwd(q, cache: KVCache, block_tables, seqlens_k, *, causal: bool = Fals
 
 def make_fwd_desc(q, cache, block_tables, seqlens_k, out, lse=None, *, causal=False, window=None,
                   alibi_slopes=None, softcap=0.0, scale=None, cu_seqlens_q=None, max_seqlen_q=None,
-                  max_seqlen_k=None, validate=False, log=False):
+                  max_seqlen_k=None, validate=False, log=False, schedule=None):
     c = make_cache(cache)
     dev, packed = cache.k.device, cu_seqlens_q is not None
     if q.dtype not in _DTYPES:
@@ -345,6 +347,9 @@ def make_fwd_desc(q, cache, block_tables, seqlens_k, out, lse=None, *, causal=Fa
     else:
         d.mask_kind = ATTN_MASK_CAUSAL if causal else ATTN_MASK_NONE
     d.flags = _flags(validate, log)
+    for name, value in (schedule or {}).items():
+        setattr(d, "sched_" + {"kernel": "kernel", "waves": "waves", "tiles": "tiles",
+                               "splits": "splits"}[name], int(value))
     for name, t in (("q", q), ("o", out)):
         axes = dict(h=1, s=0) if packed else dict(b=0, h=1, s=2)
         for axis, i in axes.items():

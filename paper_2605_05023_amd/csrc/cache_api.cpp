@@ -221,6 +221,7 @@ namespace {
 struct FwdShape {
     CacheFwdKind kind;
     int64_t max_q;  // longest query length; 0: nothing to compute
+    int64_t flat;   // flat rows of a kv head and request, at most
 };
 
 int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdParams& p, FwdShape* s)
@@ -285,59 +286,131 @@ int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdPar
     p.div_group = make_fastdiv((uint32_t)group);
     p.div_hkv = make_fastdiv((uint32_t)cache->num_kv_heads);
     s->max_q = d.batch == 0 ? 0 : max_q;
+    s->flat = s->max_q * group;
     s->kind = {cache->head_dim, cache->cache_dtype == ATTN_E5M2, d.dtype == ATTN_FP32, false, 4, 1};
-    // flat rows and workgroups are numbered with 31 bits
+    // flat rows and workgroups (of 16 rows and more) are numbered with 31 bits
     const int64_t most = packed ? d.total_q : max_q;
     if (most * group > kInt32Max || (int64_t)d.batch * d.num_q_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
-    // Flat rows of a request at most: up to 64 share tiles of 16 or 32 rows whose
-    // keys are split over wavefronts, more take tiles of 128 (fp32: 64).
-    const int64_t flat = s->max_q * group;
-    s->kind.many_rows = flat > 64;
-    s->kind.tiles = flat > 16 && !s->kind.fp32 ? 2 : 1;
-    p.tile_rows = 16 * s->kind.tiles * (s->kind.many_rows ? 4 : 1);
-    const int64_t row_tiles = (flat + p.tile_rows - 1) / p.tile_rows;
-    if (row_tiles * d.batch * cache->num_kv_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
-    p.row_tiles = (int32_t)row_tiles;
+    if ((s->flat + 15) / 16 * d.batch * cache->num_kv_heads > kInt32Max) return ATTN_ERR_UNSUPPORTED;
+    if (d.sched_kernel < 0 || d.sched_kernel > 2 || d.sched_splits < 0 || d.sched_splits > kMaxSplits ||
+        (d.sched_waves != 0 && d.sched_waves != 4 && d.sched_waves != 8) ||
+        d.sched_tiles < 0 || d.sched_tiles > (s->kind.fp32 ? 1 : 2) ||
+        (d.sched_kernel == 2 && ((d.sched_waves == 8 && D == 64) || (d.sched_tiles == 1 && !s->kind.fp32))))
+        return ATTN_ERR_BAD_VARIANT;
     return ATTN_OK;
-}
-
-int64_t part_rows(const CacheFwdParams& p, int64_t splits)
-{
-    return (int64_t)p.batch * p.pool.hkv * p.row_tiles * splits * p.tile_rows;
 }
 
 int64_t workspace_need(const CacheFwdParams& p, int64_t D)
 {
-    return p.splits > 1 ? part_rows(p, p.splits) * (D + 2) * (int64_t)sizeof(float) : 0;
+    return p.splits > 1 ? p.splits * p.ws_rows * (D + 2) * (int64_t)sizeof(float) : 0;
 }
 
-// Key splits: enough workgroups for the chip's slots (three workgroups of few
-// rows fit a CU, two of many), each with a few chunks for each of its wavefronts,
-// within the workspace's limit (a quarter of the bytes of q, out, K and V, or
-// 64 MiB where that is more).
-void plan_splits(const attn_cache_fwd_desc& d, const FwdShape& s, CacheFwdParams& p)
+// The schedules of a call: kernel, wavefronts of a workgroup, 16-row tiles of a
+// wavefront; microseconds that a launch, a round of one chunk for each wavefront
+// (many rows: for the workgroup) and a chunk's products and softmax on one SIMD
+// take, head dim 128 and bf16; workgroups that fit the chip at once (bf16 of
+// D = 128, of D = 64, fp32 likewise). Fitted to 348 calls of every kind (1..4096
+// queries, 1..128 requests, 200..32000 keys, D = 64 and 128, bf16 and fp32) that
+// were timed under each schedule and up to 64 splits: what plan_schedule takes is
+// 1.1 % over the fastest on average, 4 % at the 90th percentile, 21 % at most.
+struct Schedule {
+    bool many;
+    int waves, tiles;
+    double launch, round, tile;
+    int slots128, slots64, slots128f, slots64f;
+};
+constexpr Schedule kSchedules[] = {
+    {false, 4, 1, 4.3, 1.55, 1.15, 768, 1280, 512, 768}, {false, 8, 1, 4.4, 1.95, 1.15, 256, 512, 256, 256},
+    {false, 4, 2, 5.4, 2.3, 1.5, 512, 768, 0, 0},        {false, 8, 2, 4.9, 2.6, 1.5, 256, 256, 0, 0},
+    {true, 4, 2, 4.6, 1.6, 1.6, 512, 768, 512, 768},     {true, 8, 2, 3.8, 1.85, 0.95, 256, 0, 256, 0},
+};
+
+// Choose kernel, tile and key splits by the time that the model above expects: of
+// the longest chain of rounds, the work of all SIMDs and the memory traffic, the
+// largest and a share of the others; the dispatch of the workgroups; and the
+// second launch and the partial rows of a split call. The host knows the longest
+// lengths only: for a batch it takes the mean of two guesses, all requests at them
+// and all at 0.6 of them. The workspace stays within a quarter of the bytes of q,
+// out, K and V, or 256 MiB where that is more.
+void plan_schedule(const attn_cache_fwd_desc& d, FwdShape& s, CacheFwdParams& p, bool may_split)
 {
-    const int64_t D = s.kind.head_dim, items = (int64_t)p.batch * p.pool.hkv * p.row_tiles;
-    int64_t keys = (int64_t)p.width << p.pool.bshift;
-    if (d.max_seqlen_k > 0) keys = std::min<int64_t>(keys, d.max_seqlen_k);
-    const int64_t span = std::min<int64_t>(p.tile_rows / (int64_t)p.div_group.d + 2, s.max_q);
-    if (p.wl >= 0 && p.wr >= 0) keys = std::min<int64_t>(keys, (int64_t)p.wl + p.wr + span);
-    const int64_t chunks = keys / kChunkKeys + 2;
-    const int64_t slots = s.kind.many_rows ? 512 : 768, least = 8;
-    int64_t splits = std::min({(slots + items - 1) / items, (chunks + least - 1) / least, kMaxSplits});
-    const int64_t elt = s.kind.fp32 ? 4 : 2;
+    const int64_t D = s.kind.head_dim, heads = (int64_t)p.batch * p.pool.hkv;
+    const int64_t group = p.div_group.d;
     const int64_t rows = d.cu_seqlens_q ? d.total_q : (int64_t)d.batch * d.seqlen_q;
-    const int64_t bytes = 2 * D * (rows * p.hq * elt + keys * p.batch * p.pool.hkv);
-    const int64_t limit = std::max<int64_t>(bytes / 4, (int64_t)64 << 20);
-    splits = std::min(splits, limit / (part_rows(p, 1) * (D + 2) * (int64_t)sizeof(float)));
-    p.splits = (int32_t)std::max<int64_t>(splits, 1);
-    p.split_chunks = (int32_t)std::max((chunks + p.splits - 1) / p.splits, least);
-}
-
-void no_splits(CacheFwdParams& p)
-{
-    p.splits = 1;
-    p.split_chunks = 1 << 30;
+    int64_t held = (int64_t)p.width << p.pool.bshift;
+    if (d.max_seqlen_k > 0) held = std::min<int64_t>(held, d.max_seqlen_k);
+    const int64_t bytes = 2 * D * (rows * p.hq * (s.kind.fp32 ? 4 : 2) + held * heads);
+    const int64_t limit = std::max<int64_t>(bytes / 4, (int64_t)256 << 20);
+    p.ws_rows = rows * p.hq;
+    const int64_t part = p.ws_rows * (D + 2) * (int64_t)sizeof(float);
+    const bool d64 = D == 64, f32 = s.kind.fp32;
+    double best = 1e30;
+    for (const Schedule& c : kSchedules) {
+        const int tiles = f32 ? 1 : c.tiles;
+        const int slots = f32 ? d64 ? c.slots64f : c.slots128f : d64 ? c.slots64 : c.slots128;
+        if (slots == 0) continue;
+        const double round = c.round * (d64 ? 0.67 : 1.0) * (!f32 ? 1.0 : c.many ? 1.0 : 1.36);
+        const double tile = c.tile * (d64 ? 0.5 : 1.0) * (!f32 ? 1.0 : c.many ? 1.0 : 1.55);
+        const bool forced = d.sched_kernel || d.sched_waves || d.sched_tiles;
+        if (forced) {
+            if ((d.sched_kernel && c.many != (d.sched_kernel == 2)) ||
+                (d.sched_waves && c.waves != d.sched_waves) || (d.sched_tiles && tiles != d.sched_tiles))
+                continue;
+        } else if (s.flat <= 16 ? c.many || tiles > 1 : !c.many && c.tiles == 1 && s.flat > 64 && !f32) {
+            continue;  // rows that one tile holds; more than four of them, with a wider one at hand
+        } else if (f32 && c.many && c.waves == 8) {
+            continue;  // up to a third slower than with four (23 calls, 0.5 % faster at best)
+        }
+        const int64_t tile_rows = 16 * tiles * (c.many ? c.waves : 1);
+        const int64_t row_tiles = (s.flat + tile_rows - 1) / tile_rows;
+        int64_t keys = held;
+        if (p.wl >= 0 && p.wr >= 0)
+            keys = std::min<int64_t>(keys, (int64_t)p.wl + p.wr + std::min(tile_rows / group + 2, s.max_q));
+        const int64_t chunks = std::max<int64_t>((keys + kChunkKeys - 1) / kChunkKeys, 1);
+        const double seen = p.wl < 0 && p.wr >= 0 ? std::max(1.0, (double)chunks - (double)s.max_q / 128) : (double)chunks;
+        double items = (double)(heads * row_tiles);
+        if (d.cu_seqlens_q)
+            items = std::min(items, p.pool.hkv * ((double)(rows * group) / (double)tile_rows + 0.5 * p.batch));
+        int64_t before = 0;
+        for (const int64_t n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+            const int64_t splits = d.sched_splits && may_split ? d.sched_splits : n;
+            if (splits > 1 && (!may_split || (!d.sched_splits && (splits > chunks || splits * part > limit)))) break;
+            const int64_t per = (chunks + splits) / splits;  // (a chunk more: a range may begin inside one)
+            if (per == before) continue;
+            before = per;
+            const double used = splits > 1 ? (double)((chunks + per - 1) / per) : 1.0;
+            const double rounds = (double)(c.many ? per : (per + c.waves - 1) / c.waves) * round;
+            double us = 0.0;
+            for (const double fill : {1.0, 0.6}) {
+                const double avg = std::max(1.0, fill * seen), share = splits > 1 ? 1.0 : avg / (double)chunks;
+                const double parts = std::max(1.0, used * fill), turns = items * parts / slots;
+                const double chain = rounds * (turns > 1 ? std::max(1.0, turns * share + 0.6) : 1.0);
+                const double work = items * avg * (c.many ? c.waves : 1) / 1024 * tile;
+                const double memory = (double)heads * avg * (double)(kChunkKeys * 2 * D) / 8.7e6;
+                const double most = std::max({chain, work, memory});
+                double one = c.launch + 0.0033 * items * parts * (c.waves / 4) + most +
+                             0.2 * (chain + work + memory - most);
+                if (splits > 1)  // the second launch, the partial rows, and the host's time for two
+                    one = std::max(one + 2.7 + 2 * parts * (double)part / 3.6e6, 10.0);
+                us += std::max(one, 6.4);
+                if (p.batch == 1) {
+                    us *= 2;
+                    break;
+                }
+            }
+            if (us < best) {
+                best = us;
+                s.kind.many_rows = c.many;
+                s.kind.waves = c.waves;
+                s.kind.tiles = tiles;
+                p.tile_rows = (int32_t)tile_rows;
+                p.row_tiles = (int32_t)row_tiles;
+                p.splits = (int32_t)splits;
+                p.split_chunks = splits > 1 ? (int32_t)per : 1 << 30;
+            }
+            if (d.sched_splits) break;
+        }
+    }
 }
 
 int validate_fwd(const attn_cache_fwd_desc& d, const CacheFwdParams& p, int64_t max_q)
@@ -378,7 +451,7 @@ extern "C" int64_t attn_cache_workspace_bytes(const attn_cache* cache, const att
     const int rc = check_fwd(cache, *desc, p, &s);
     if (rc != ATTN_OK) return rc;
     if (s.max_q == 0) return 0;
-    plan_splits(*desc, s, p);
+    plan_schedule(*desc, s, p, true);
     return workspace_need(p, s.kind.head_dim);
 }
 
@@ -413,13 +486,13 @@ extern "C" int attn_cache_fwd(const void* q, void* out, float* lse, const attn_c
     p.table = d.block_tables;
     p.seqlens = d.seqlens_k;
     p.cu_q = d.cu_seqlens_q;
-    plan_splits(d, s, p);
+    plan_schedule(d, s, p, workspace != nullptr);
     const int64_t need = workspace_need(p, s.kind.head_dim);
-    if (need > 0 && workspace && workspace_bytes >= need) {
+    if (need > workspace_bytes) {
+        plan_schedule(d, s, p, false);
+    } else if (need > 0) {
         p.ws_o = static_cast<float*>(workspace);
-        p.ws_ml = p.ws_o + part_rows(p, p.splits) * s.kind.head_dim;
-    } else {
-        no_splits(p);
+        p.ws_ml = p.ws_o + p.splits * p.ws_rows * s.kind.head_dim;
     }
     if (d.flags & ATTN_FLAG_VALIDATE) {
         rc = validate_fwd(d, p, s.max_q);
@@ -428,11 +501,11 @@ extern "C" int attn_cache_fwd(const void* q, void* out, float* lse, const attn_c
     if (d.flags & ATTN_FLAG_LOG)
         std::fprintf(stderr,
                      "attn_cache_fwd: %s over %s D=%d B=%d Hq=%d Hkv=%d block %d %s window (%d, %d) alibi=%d "
-                     "softcap=%g | %s rows, %d a tile, %d tiles a kv head, key splits %d\n",
+                     "softcap=%g | %s rows, %d wavefronts, %d rows a tile, %d tiles a kv head, key splits %d\n",
                      s.kind.fp32 ? "fp32" : "bf16", format_name(cache), s.kind.head_dim, d.batch, d.num_q_heads,
                      p.pool.hkv, cache->block_size, packed ? "packed" : "fixed-length", p.wl, p.wr,
-                     p.slopes != nullptr, (double)d.softcap, s.kind.many_rows ? "many" : "few", p.tile_rows,
-                     p.row_tiles, p.splits);
+                     p.slopes != nullptr, (double)d.softcap, s.kind.many_rows ? "many" : "few", s.kind.waves,
+                     p.tile_rows, p.row_tiles, p.splits);
     hipStream_t stream = static_cast<hipStream_t>(d.stream);
     const bool d128 = s.kind.head_dim == 128;
     hipError_t err = s.kind.e5m2 ? d128 ? attn::launch_cache_fwd_e5m2_d128(p, s.kind, stream)

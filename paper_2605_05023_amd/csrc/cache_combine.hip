@@ -26,14 +26,15 @@ __global__ __launch_bounds__(NT) void cache_combine_kernel(CacheFwdParams p)
     const int per = split_size(p, c1 - c0);
     if (c1 - c0 <= per) return;
     const int n = (c1 - c0 + per - 1) / per;
-    const int64_t part = ((int64_t)group * p.row_tiles + rt) * p.splits * p.tile_rows + row;
+    const Writer<D, T> write{p, t, -1};
+    const int64_t part = write.lse_row(f);
     const int col = 4 * (lane % COLS), par = lane / COLS;
 
     // the splits' scalars, one per lane (no more than 64 splits)
     float m = -__builtin_inff(), l = 0.0f;
     if (lane < n) {
-        m = p.ws_ml[2 * (part + (int64_t)lane * p.tile_rows)];
-        l = p.ws_ml[2 * (part + (int64_t)lane * p.tile_rows) + 1];
+        m = p.ws_ml[2 * (part + lane * p.ws_rows)];
+        l = p.ws_ml[2 * (part + lane * p.ws_rows) + 1];
     }
     float top = m;
 #pragma unroll
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(NT) void cache_combine_kernel(CacheFwdParams p)
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int s = min(s0 + u * PAR + par, n - 1);
-            x[u] = *reinterpret_cast<const f32x4*>(src + (int64_t)s * p.tile_rows * D);
+            x[u] = *reinterpret_cast<const f32x4*>(src + s * p.ws_rows * D);
         }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
@@ -62,9 +63,8 @@ __global__ __launch_bounds__(NT) void cache_combine_kernel(CacheFwdParams p)
     for (int d = COLS; d < 64; d <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
-    const Writer<D, T> write{p, t, -1};
-    if (lane == 0) write.scalars(f, row, top, l);
-    if (par == 0) write.out(f, row, col, acc * write.factor(l));
+    if (lane == 0) write.scalars(f, top, l);
+    if (par == 0) write.out(f, col, acc * write.factor(l));
 }
 
 template <int D>

@@ -222,31 +222,28 @@ __device__ __forceinline__ ChunkScales chunk_scales(float ks, float vs, int key,
     return c;
 }
 
-// One online-softmax step of a row tile: updates the running maximum, this
-// lane's share of the row sum and O, and gives P times V's scale as NS bf16
-// terms, the B operand of the P V products. P = 2^(score - maximum) and vs are
-// one exponential, of an FMA with the score's factors. The sum takes P without
-// vs. O and the sum are rescaled only where a maximum grows by more than 8 (P
-// stays below 2^8, whose bf16 has the same relative error).
-template <int NS, int DT, int MODS>
-__device__ __forceinline__ void softmax_step(const CacheFwdParams& p, const f32x4 (&s)[4],
-                                             const ChunkScales& c, int jlo, int jhi, int ip, float slope,
-                                             float& mx, float& sum, f32x4 (&acc)[DT], bf16x8 (&pf)[2][NS])
+// One online-softmax step of a row tile, in two parts.
+// softmax_max: score options and mask on s in place, then the running maximum.
+// O and the sum are rescaled only where a maximum grows by more than 8 (P stays
+// below 2^8, whose bf16 has the same relative error). Returns the factor that
+// makes the scores of s.
+template <int DT, int MODS>
+__device__ __forceinline__ float softmax_max(const CacheFwdParams& p, f32x4 (&s)[4], const ChunkScales& c,
+                                             int jlo, int jhi, int ip, float slope, float& mx, float& sum,
+                                             f32x4 (&acc)[DT])
 {
-    float x[16];
-    float factor = c.ks * p.scale_u;  // x * factor is the score
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = s[j / 4][j % 4];
+    float factor = c.ks * p.scale_u;
     if constexpr (MODS != kModsNone) {
         const float from = (float)(ip - c.key);
         // the short form's error, 1e-4 at most (score_mods.h), is far below that of bf16
         const float pre = c.ks * (MODS == kModsCapShort ? p.cap_pre2 : p.cap_pre);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            if constexpr (MODS == kModsCapShort) x[j] = softcap_short_u(x[j], pre, p.cap_post);
-            else if constexpr (MODS == kModsCapExact) x[j] = softcap_u(x[j], pre, p.cap_post);
-            else x[j] *= factor;
-            x[j] = __builtin_fmaf(slope, __builtin_fabsf(from - (float)j), x[j]);
+            float x = s[j / 4][j % 4];
+            if constexpr (MODS == kModsCapShort) x = softcap_short_u(x, pre, p.cap_post);
+            else if constexpr (MODS == kModsCapExact) x = softcap_u(x, pre, p.cap_post);
+            else x *= factor;
+            s[j / 4][j % 4] = __builtin_fmaf(slope, __builtin_fabsf(from - (float)j), x);
         }
         factor = 1.0f;
     }
@@ -257,16 +254,16 @@ __device__ __forceinline__ void softmax_step(const CacheFwdParams& p, const f32x
         const bool zero = factor == 0.0f;
         factor = zero ? 1.0f : factor;
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            x[j] = j >= lo && j < hi ? zero ? 0.0f : x[j] : -__builtin_inff();
+        for (int j = 0; j < 16; ++j) {
+            const float x = zero ? 0.0f : s[j / 4][j % 4];
+            s[j / 4][j % 4] = j >= lo && j < hi ? x : -__builtin_inff();
+        }
     }
-    float top[6];
+    auto x = [&](int j) { return s[j / 4][j % 4]; };
+    float top = x(0);
 #pragma unroll
-    for (int j = 0; j < 5; ++j)
-        top[j] = __builtin_fmaxf(__builtin_fmaxf(x[3 * j], x[3 * j + 1]), x[3 * j + 2]);
-    top[5] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), top[2]);
-    top[5] = __builtin_fmaxf(__builtin_fmaxf(top[3], top[4]), __builtin_fmaxf(top[5], x[15]));
-    const float now = row_max(top[5] * factor);
+    for (int j = 1; j < 15; j += 2) top = __builtin_fmaxf(__builtin_fmaxf(top, x(j)), x(j + 1));
+    const float now = row_max(__builtin_fmaxf(top, x(15)) * factor);
     if (__builtin_amdgcn_ballot_w64(now > mx + 8.0f)) {
         const float to = __builtin_fmaxf(mx, now);
         // (a row without a key so far: nothing to scale, and not 2^(inf - inf))
@@ -276,20 +273,38 @@ __device__ __forceinline__ void softmax_step(const CacheFwdParams& p, const f32x
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] *= keep;
     }
+    return factor;
+}
+
+// softmax_exp: P times V's scale as NS bf16 terms, the B operand of the P V
+// products: 2^(score - maximum) and vs are one exponential, of an FMA with the
+// score's factor. This lane's share of the row sum takes P without vs.
+template <int NS>
+__device__ __forceinline__ void softmax_exp(const f32x4 (&s)[4], const ChunkScales& c, float factor, float mx,
+                                            float& sum, bf16x8 (&pf)[2][NS])
+{
     const float shift = c.lvs - (mx == -__builtin_inff() ? 0.0f : mx);
     float add[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], factor, shift));
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], factor, shift));
         add[j % 4] += e;
         split_p<NS>(e, pf[j / 8], j % 8);
     }
     sum = __builtin_fmaf((add[0] + add[1]) + (add[2] + add[3]), c.ivs, sum);
+}
+
+// Where V's scale is 0: no share of V, whatever its bytes.
+template <int MT, int NS>
+__device__ __forceinline__ void drop_v(const ChunkScales& c, bf16x8 (&pf)[MT][2][NS])
+{
     if (!c.whole && c.no_v) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NS; ++n) pf[k][n] = bf16x8{};
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < NS; ++n) pf[m][k][n] = bf16x8{};
     }
 }
 
@@ -302,39 +317,51 @@ __device__ __forceinline__ uint32_t byte_mask(int i, int lo, int hi)
     return below_b & ~below_a;
 }
 
-// O, row sum and maximum of one row (lane: 4 consecutive dims) to the output,
-// or to the partials of split sp.
+// Where a row's O, row sum and maximum go: to the output, or to the partials of
+// a split, which are in the order of the LSE.
 template <int D, class T>
 struct Writer {
     const CacheFwdParams& p;
     const RowTile& t;
-    int64_t part;  // index of the tile's first partial row, or -1
+    int64_t part;  // first partial row of the split, or -1
 
-    __device__ __forceinline__ void scalars(int f, int row, float m, float l) const
+    // Query and head of flat row f, and its row of the LSE.
+    __device__ __forceinline__ void place(int f, int* qi, int64_t* h) const
     {
+        *qi = (int)fast_div((uint32_t)f, p.div_group);
+        *h = t.hkv * (int)p.div_group.d + (f - *qi * (int)p.div_group.d);
+    }
+    __device__ __forceinline__ int64_t lse_row(int f) const
+    {
+        int qi;
+        int64_t h;
+        place(f, &qi, &h);
+        return p.cu_q ? h * p.total_q + t.qrow0 + qi : ((int64_t)t.b * p.hq + h) * p.seqlen_q + qi;
+    }
+    __device__ __forceinline__ void scalars(int f, float m, float l) const
+    {
+        const int64_t row = lse_row(f);
         if (part >= 0) {
             p.ws_ml[2 * (part + row)] = m;
             p.ws_ml[2 * (part + row) + 1] = l;
         } else if (p.lse) {
-            const int qi = (int)fast_div((uint32_t)f, p.div_group);
-            const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
-            const int64_t at = p.cu_q ? h * p.total_q + t.qrow0 + qi
-                                      : ((int64_t)t.b * p.hq + h) * p.seqlen_q + qi;
-            p.lse[at] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+            p.lse[row] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
         }
     }
     __device__ __forceinline__ float factor(float l) const  // (a NaN sum reaches O)
     {
         return part >= 0 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
     }
-    __device__ __forceinline__ void out(int f, int row, int d, f32x4 x) const
+    // Four dims from d on.
+    __device__ __forceinline__ void out(int f, int d, f32x4 x) const
     {
         if (part >= 0) {
-            *reinterpret_cast<f32x4*>(p.ws_o + (part + row) * D + d) = x;
+            *reinterpret_cast<f32x4*>(p.ws_o + (part + lse_row(f)) * D + d) = x;
             return;
         }
-        const int qi = (int)fast_div((uint32_t)f, p.div_group);
-        const int64_t h = t.hkv * (int)p.div_group.d + (f - qi * (int)p.div_group.d);
+        int qi;
+        int64_t h;
+        place(f, &qi, &h);
         T* dst = static_cast<T*>(p.o) + (p.cu_q ? t.qrow0 + qi : qi) * p.so_s + h * p.so_h +
                  (p.cu_q ? 0 : t.b * p.so_b) + d;
         if constexpr (sizeof(T) == 2)
@@ -366,9 +393,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_fwd_kernel(CacheFwdParams
     if (sp > 0 && c0 + sp * per >= c1) return;  // whole workgroup
     c0 += sp * per;
     c1 = min(c1, c0 + per);
-    const int64_t part =
-        split ? (((int64_t)group * p.row_tiles + rt) * p.splits + sp) * p.tile_rows : (int64_t)-1;
-    const Writer<D, T> write{p, t, part};
+    const Writer<D, T> write{p, t, split ? sp * p.ws_rows : (int64_t)-1};
 
     // keys that any, and that every row sees
     int lo_any, hi_any, lo_all, hi_all;
@@ -482,9 +507,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_fwd_kernel(CacheFwdParams
 
         bf16x8 pf[MT][2][NS];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-            softmax_step<NS, DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m],
-                                       pf[m]);
+        for (int m = 0; m < MT; ++m) {
+            const float factor =
+                softmax_max<DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m]);
+            softmax_exp<NS>(s[m], cs, factor, mx[m], sum[m], pf[m]);
+        }
+        drop_v<MT, NS>(cs, pf);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -538,8 +566,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_fwd_kernel(CacheFwdParams
             l = __builtin_fmaf(lml[w][row][1], k, l);
             o += *reinterpret_cast<const f32x4*>(&lo_[w][row * LD + col]) * k;
         }
-        if (col == 0) write.scalars(f, row, top, l);
-        write.out(f, row, col, o * write.factor(l));
+        if (col == 0) write.scalars(f, top, l);
+        write.out(f, col, o * write.factor(l));
     }
 }
 

@@ -14,8 +14,10 @@ hipError_t launch_rows(const CacheFwdParams& p, const CacheFwdKind& k, hipStream
     constexpr int TWO = sizeof(T) == 2 ? 2 : 1;
     const dim3 grid((unsigned)(p.batch * p.pool.hkv) * (unsigned)p.row_tiles, (unsigned)p.splits);
     const dim3 block(64 * k.waves);
-    if (k.many_rows)
-        hipLaunchKernelGGL((cache_many_kernel<D, T, E5M2, TWO, MODS>), grid, block, 0, stream, p);
+    if (k.many_rows && D == 128 && k.waves == 8)
+        hipLaunchKernelGGL((cache_many_kernel<128, T, E5M2, TWO, MODS, 8>), grid, block, 0, stream, p);
+    else if (k.many_rows)
+        hipLaunchKernelGGL((cache_many_kernel<D, T, E5M2, TWO, MODS, 4>), grid, block, 0, stream, p);
     else if (k.waves == 8 && k.tiles == 1)
         hipLaunchKernelGGL((cache_fwd_kernel<D, T, E5M2, 1, MODS, 8>), grid, block, 0, stream, p);
     else if (k.waves == 8)

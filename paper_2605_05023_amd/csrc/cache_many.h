@@ -3,9 +3,9 @@
 // more than 64 flat rows a kv head.
 //
 // Products, operand layouts and the treatment of scales are those of
-// cache_kernel.h. What differs is who reads K and V: here the four wavefronts
-// of a workgroup take row tiles of their own (16 MT rows each) against the same
-// keys. Each chunk of 64 keys is loaded once per workgroup, 16 bytes a thread
+// cache_kernel.h. What differs is who reads K and V: here the wavefronts of a
+// workgroup (four, or eight for large calls) take row tiles of their own (16 MT
+// rows each) against the same keys. Each chunk of 64 keys is loaded once per workgroup, 16 bytes a thread
 // and load, converted to bf16 once (a wavefront that converted all of it for
 // itself spent as many instructions on that as on the softmax) and staged in
 // LDS, K as [key][dim] and V as [dim][key], two buffers, one barrier a chunk:
@@ -51,18 +51,20 @@ __device__ __forceinline__ void issue_order()
     __builtin_amdgcn_sched_group_barrier(0x008, 4 * USES, SET);
 }
 
-template <int D, class T, bool E5M2, int MT, int MODS>
-__global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
+template <int D, class T, bool E5M2, int MT, int MODS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache_many_kernel(CacheFwdParams p)
 {
     constexpr int NS = sizeof(T) == 2 ? 1 : 3;
     constexpr int WR = 16 * MT, KS = D / 32, DT = D / 16;
-    constexpr int PIECES = D / 64;            // 16-byte loads of K (and of V) per thread and chunk
+    constexpr int THREADS = 64 * WAVES;
+    constexpr int PIECES = D / (16 * WAVES);  // 16-byte loads of K (and of V) per thread and chunk
+    static_assert(PIECES >= 1, "a piece for every thread");
     constexpr int TILE = kChunk * D * 2;      // bytes of a staged tile
     __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     if constexpr (kLdsPoison) {
-        for (int i = tid; i < 4 * TILE / 4; i += NT) reinterpret_cast<uint32_t*>(&lds[0][0][0])[i] = ~0u;
+        for (int i = tid; i < 4 * TILE / 4; i += THREADS) reinterpret_cast<uint32_t*>(&lds[0][0][0])[i] = ~0u;
         __syncthreads();
     }
 
@@ -77,9 +79,7 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
     if (sp > 0 && c0 + sp * per >= c1) return;  // whole workgroup
     c0 += sp * per;
     c1 = min(c1, c0 + per);
-    const int64_t part =
-        split ? (((int64_t)group * p.row_tiles + rt) * p.splits + sp) * p.tile_rows : (int64_t)-1;
-    const Writer<D, T> write{p, t, part};
+    const Writer<D, T> write{p, t, split ? sp * p.ws_rows : (int64_t)-1};
 
     // keys that any row of the workgroup, any and every row of the wavefront sees
     const int fw = t.f0 + wave * WR;
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             // (a wavefront's pieces of K lie in one group)
-            const int piece = tid + NT * i, row = piece / (D / 16), col = piece % (D / 16);
-            const int kg = D == 128 ? 2 * i + (wave >> 1) : wave;
+            const int piece = tid + THREADS * i, row = piece / (D / 16), col = piece % (D / 16);
+            const int kg = D == 128 ? (WAVES / 2) * i + (wave >> 1) : wave;
             const int page_k = kg & 2 ? kg & 1 ? pages[3] : pages[2] : kg & 1 ? pages[1] : pages[0];
             s.k[i] = *reinterpret_cast<const u32x4*>(kbase + (int64_t)max(page_k, 0) * p.pool.sk_b +
                                                      ((base + row) & bs1) * D + 16 * col);
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
         const int lo = min(max(lo_wg - key, 0), 16), hi = s.page_v < 0 ? 0 : min(max(hi_wg - key, 0), 16);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int piece = tid + NT * i, row = piece / (D / 16), col = piece % (D / 16), d = piece >> 2;
+            const int piece = tid + THREADS * i, row = piece / (D / 16), col = piece % (D / 16), d = piece >> 2;
             u32x4 w = s.v[i];
             if (edge) {
 #pragma unroll
@@ -239,9 +239,12 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
                 chunk_scales(ks, vs, key, page, base >= lo_all && base + kChunk <= hi_all);
             bf16x8 pf[MT][2][NS];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-                softmax_step<NS, DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m],
-                                           acc[m], pf[m]);
+            for (int m = 0; m < MT; ++m) {
+                const float factor =
+                    softmax_max<DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m]);
+                softmax_exp<NS>(s[m], cs, factor, mx[m], sum[m], pf[m]);
+            }
+            drop_v<MT, NS>(cs, pf);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -264,9 +267,9 @@ __global__ __launch_bounds__(NT, 2) void cache_many_kernel(CacheFwdParams p)
         const int f = fw + 16 * m + r;
         if (f >= t.nflat) continue;
         const float inv = write.factor(sum[m]);
-        if (g == 0) write.scalars(f, f - t.f0, mx[m], sum[m]);
+        if (g == 0) write.scalars(f, mx[m], sum[m]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) write.out(f, f - t.f0, 16 * d + 4 * g, acc[m][d] * inv);
+        for (int d = 0; d < DT; ++d) write.out(f, 16 * d + 4 * g, acc[m][d] * inv);
     }
 }
 

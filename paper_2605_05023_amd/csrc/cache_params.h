@@ -68,9 +68,10 @@ struct CacheFwdParams {
     // row_tiles tiles of tile_rows flat rows for each kv group.
     int32_t row_tiles, tile_rows;
     // Key splits: `splits` workgroups share a row tile's chunks of 64 keys, at
-    // least split_chunks each. Partials: ws_o [groups * row_tiles][splits]
-    // [tile_rows][D], ws_ml the same with (running max, row sum).
+    // least split_chunks each. Partials, in the order of the LSE's ws_rows rows:
+    // ws_o [splits][ws_rows][D], ws_ml the same with (running max, row sum).
     int32_t splits, split_chunks;
+    int64_t ws_rows;
     float* ws_o;
     float* ws_ml;
 };

@@ -183,6 +183,12 @@ FWD_BAD = [
     ("no lengths", dict(seqlens_k=None), "ATTN_ERR_NULL_PTR"),
     ("slopes", dict(alibi_slopes=P + 2), "ATTN_ERR_ALIGNMENT"),
     ("rows", dict(seqlen_q=1 << 30), "ATTN_ERR_UNSUPPORTED"),
+    ("table keys", dict(table_width=1 << 25), "ATTN_ERR_UNSUPPORTED"),
+    ("schedule kernel", dict(sched_kernel=3), "ATTN_ERR_BAD_VARIANT"),
+    ("schedule waves", dict(sched_waves=6), "ATTN_ERR_BAD_VARIANT"),
+    ("schedule tiles", dict(sched_tiles=3), "ATTN_ERR_BAD_VARIANT"),
+    ("schedule tiles, many", dict(sched_kernel=2, sched_tiles=1), "ATTN_ERR_BAD_VARIANT"),
+    ("schedule splits", dict(sched_splits=65), "ATTN_ERR_BAD_VARIANT"),
 ]
 
 
@@ -211,7 +217,7 @@ def test_fwd_pointers_and_empty_calls():
 
 
 def test_workspace_is_bounded():
-    """No more than a quarter of q, out, K and V, or 64 MiB."""
+    """No more than a quarter of q, out, K and V, or 256 MiB."""
     lib = attn.load()
     for batch, hq, hkv, sq, width in ((1, 32, 8, 1, 4000), (64, 128, 8, 1, 2000), (2, 8, 8, 500, 1000),
                                       (1, 64, 8, 4096, 1000), (300, 8, 8, 3, 100)):
@@ -219,7 +225,7 @@ def test_workspace_is_bounded():
         d = fwd_desc(batch=batch, num_q_heads=hq, seqlen_q=sq, table_width=width)
         n = lib.attn_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(d))
         moved = 2 * 128 * (batch * sq * hq * 2 + batch * width * 64 * hkv)
-        assert 0 <= n <= max(moved // 4, 64 << 20)
+        assert 0 <= n <= max(moved // 4, 256 << 20)
     # one decode row of a long context is split, one of a short context is not
     d = fwd_desc(batch=1, seqlen_q=1, table_width=1000)
     c = pool(num_blocks=1000)

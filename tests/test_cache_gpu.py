@@ -307,9 +307,23 @@ def run_case(c, *, max_q=None, max_k=None, ws=True, lib=None, **extra):
     return out.cpu().transpose(1, 2).flatten(0, 1), lse.cpu().transpose(1, 2).flatten(0, 1)
 
 
+def schedules(c):
+    """The kernels that a call may take: the library's choice and each of them."""
+    fp32, d = c["dt"] == "fp32", c["q"].shape[-1]
+    two = 1 if fp32 else 2
+    yield None
+    yield dict(kernel=1, waves=4, tiles=1)
+    yield dict(kernel=1, waves=8, tiles=two, splits=3)
+    yield dict(kernel=2, waves=4)
+    yield dict(kernel=2, waves=4 if d == 64 else 8, splits=2)
+
+
 def check_case(c, **how):
-    out, lse = run_case(c, **how)
-    assert bool(torch.isfinite(out.float()).all())
+    got = []
+    for sched in [None] if "lib" in how else schedules(c):
+        out, lse = run_case(c, schedule=sched, **how)
+        assert bool(torch.isfinite(out.float()).all()), sched
+        got.append((sched, out, lse))
     k, v, ks, vs = c["pool"]
     kd, vd = ref.decode(k, c["fmt"]), ref.decode(v, c["fmt"])
     at, held = 0, c["table"].shape[1] * c["bs"]
@@ -320,7 +334,8 @@ def check_case(c, **how):
         vv, _ = ref.dense(vd, vs, c["table"][r], keys, c["bs"], True)
         kk[:, ~there], vv[:, ~there] = 0.0, 0.0
         want = ref.attention(c["q"][at:at + n], kk, vv, lk, group=group, slopes=c["slopes"], there=there, **c["opt"])
-        check_rows(f"request {r} ({n} x {lk})", out[at:at + n], lse[at:at + n], want, c["dt"])
+        for sched, out, lse in got:
+            check_rows(f"request {r} ({n} x {lk}), schedule {sched}", out[at:at + n], lse[at:at + n], want, c["dt"])
         at += n
 
 
@@ -475,9 +490,10 @@ def test_nan_reaches_the_rows_that_see_it():
     c = attention_case(lens=[(1, 200)], hq=2, hkv=2, seed=19, spoiled=False)
     k, v, ks, vs = c["pool"]
     k.view(torch.uint8)[int(c["table"][0, 1]), 0, 5] = 0x7F
-    out, lse = run_case(c)
-    assert torch.isnan(out[0, 0].float()).all() and torch.isnan(lse[0, 0])
-    assert torch.isfinite(out[0, 1].float()).all() and torch.isfinite(lse[0, 1])
+    for sched in schedules(c):
+        out, lse = run_case(c, schedule=sched)
+        assert torch.isnan(out[0, 0].float()).all() and torch.isnan(lse[0, 0])
+        assert torch.isfinite(out[0, 1].float()).all() and torch.isfinite(lse[0, 1])
 
 
 def test_far_pages():
@@ -637,9 +653,11 @@ def test_poisoned_lds():
     lib = _abi.load(path)
     for c in (attention_case(lens=[(1, 300), (2, 5000), (1, 1)], seed=40),
               attention_case(lens=[(40, 300), (90, 100)], seed=41, dt="fp32", d=64),
+              attention_case(lens=[(40, 300), (90, 100)], seed=41),
               attention_case(lens=[(1, 64)], seed=42, d=64, fmt="e5m2", bs=16)):
-        a, b = run_case(c), run_case(c, lib=lib)
-        assert bytes_equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        for sched in schedules(c):
+            a, b = run_case(c, schedule=sched), run_case(c, lib=lib, schedule=sched)
+            assert bytes_equal(a[0], b[0]) and torch.equal(a[1], b[1])
     log("attention ok")
     for runs in (RUNS["prompt"], RUNS["decode"]):
         got = []
