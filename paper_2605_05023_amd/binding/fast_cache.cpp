@@ -85,6 +85,16 @@ void* stream_of(const at::Device& dev) { return c10::hip::getCurrentHIPStream(de
 
 bool handled(int status) { return status == ATTN_OK || status == ATTN_ERR_LAUNCH; }
 
+// A contiguous tensor of n entries in the storage of `base` (bytes), `at` bytes on.
+at::Tensor part_of(const at::Tensor& base, int64_t at, int64_t n, const caffe2::TypeMeta& type)
+{
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), type);
+    c10::TensorImpl* impl = t.unsafeGetTensorImpl();
+    impl->set_storage_offset(at / (int64_t)type.itemsize());
+    impl->set_sizes_contiguous({n});
+    return t;
+}
+
 enum PlanArg { pCached, pNew, pTable, pFree, pNumFree, pBlock, pTotal, pArgs };
 
 bool plan(PyObject* const* a, at::Tensor out[4], int* status)
@@ -103,11 +113,14 @@ bool plan(PyObject* const* a, at::Tensor out[4], int* status)
     if (d.total_new < 0 || d.total_new > INT32_MAX) return false;
     const NoGil nogil;
     at::AutoDispatchBelowADInplaceOrView below;
-    const auto i32 = cached.options();
-    out[0] = at::empty({d.total_new}, i32.dtype(at::kLong));
-    out[1] = at::empty({batch + 1}, i32);
-    out[2] = at::empty({batch}, i32);
-    out[3] = at::empty({1}, i32);
+    // one allocation for the four (each costs 0.8 us of 7.6 a call)
+    const auto i32 = caffe2::TypeMeta::Make<int32_t>();
+    const int64_t slots = 8 * d.total_new;
+    const at::Tensor all = at::empty({slots + 4 * (2 * batch + 2)}, cached.options().dtype(at::kByte));
+    out[0] = part_of(all, 0, d.total_new, caffe2::TypeMeta::Make<int64_t>());
+    out[1] = part_of(all, slots, batch + 1, i32);
+    out[2] = part_of(all, slots + 4 * (batch + 1), batch, i32);
+    out[3] = part_of(all, slots + 4 * (2 * batch + 1), 1, i32);
     d.batch = (int32_t)batch;
     d.free_len = (int32_t)free_blocks.numel();
     d.cached_lens = cached.const_data_ptr<int32_t>();

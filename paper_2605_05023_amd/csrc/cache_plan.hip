@@ -17,25 +17,24 @@ namespace {
 
 constexpr int NT = 256, kReqs = 64;
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v)
+// Inclusive prefix sum over the wavefront, without LDS: shifts within rows of 16
+// lanes, then the last lane of each row (row pair) to the rows behind it.
+__device__ __forceinline__ int32_t wave_scan(int32_t v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
     return v;
 }
+__device__ __forceinline__ int32_t last_lane(int32_t v) { return __builtin_amdgcn_readlane(v, 63); }
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane)  // inclusive
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t u = __shfl_up(v, d);
-        if (lane >= d) v += u;
-    }
-    return v;
-}
-
+// The sums of new tokens, and so of blocks, stay below 2^31; lengths that break
+// that give wrong slots, but no access out of range.
 struct Request {
-    int64_t cached, fresh, need;
+    int32_t cached, fresh, need;
     bool fits;
 };
 
@@ -45,14 +44,14 @@ __device__ __forceinline__ Request request(const CachePlanParams& p, int r)
     q.cached = max(p.cached[r], 0);
     q.fresh = max(p.fresh[r], 0);
     const int64_t b1 = (1 << p.bshift) - 1;
-    const int64_t last = (q.cached + q.fresh + b1) >> p.bshift;
+    const int64_t last = ((int64_t)q.cached + q.fresh + b1) >> p.bshift;
     q.fits = last <= p.width;
-    q.need = q.fits ? last - ((q.cached + b1) >> p.bshift) : 0;
+    q.need = q.fits ? (int32_t)(last - ((q.cached + b1) >> p.bshift)) : 0;
     return q;
 }
 
 // Largest i < n with start[i] <= x (start ascending, start[0] <= x).
-__device__ __forceinline__ int find(const int64_t* start, int n, int64_t x)
+__device__ __forceinline__ int find(const int32_t* start, int n, int32_t x)
 {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
@@ -65,8 +64,8 @@ __device__ __forceinline__ int find(const int64_t* start, int n, int64_t x)
 
 __global__ __launch_bounds__(NT) void cache_plan_kernel(CachePlanParams p)
 {
-    __shared__ int64_t sum[2][NT / 64];
-    __shared__ int64_t tok[kReqs + 1], blk[kReqs + 1];  // prefix sums, those before included
+    __shared__ int32_t sum[2][NT / 64];
+    __shared__ int32_t tok[kReqs + 1], blk[kReqs + 1];  // prefix sums, those before included
     __shared__ int32_t held[kReqs];
     __shared__ int32_t granted[kReqs];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -79,16 +78,19 @@ __global__ __launch_bounds__(NT) void cache_plan_kernel(CachePlanParams p)
     }
     const int first = (int)blockIdx.x * kReqs, n = min(kReqs, p.batch - first);
     const bool last_x = blockIdx.x == gridDim.x - 1;
-    const int64_t avail = min(max(*p.num_free, 0), p.free_len);
+    const int32_t avail = min(max(*p.num_free, 0), p.free_len);
+    Request q = {0, 0, 0, true};
+    if (lane < n) q = request(p, first + lane);
 
-    int64_t t = 0, b = 0;
+    int32_t t = 0, b = 0;
+#pragma unroll 4
     for (int r = tid; r < first; r += NT) {
-        const Request q = request(p, r);
-        t += q.fresh;
-        b += q.need;
+        const Request e = request(p, r);
+        t += e.fresh;
+        b += e.need;
     }
-    t = wave_sum(t);
-    b = wave_sum(b);
+    t = last_lane(wave_scan(t));
+    b = last_lane(wave_scan(b));
     if (lane == 0) {
         sum[0][wave] = t;
         sum[1][wave] = b;
@@ -101,9 +103,7 @@ __global__ __launch_bounds__(NT) void cache_plan_kernel(CachePlanParams p)
             t += sum[0][w];
             b += sum[1][w];
         }
-        Request q = {0, 0, 0, true};
-        if (lane < n) q = request(p, first + lane);
-        const int64_t te = t + wave_scan(q.fresh, lane), be = b + wave_scan(q.need, lane);
+        const int32_t te = t + wave_scan(q.fresh), be = b + wave_scan(q.need);
         const bool ok = q.fits && (q.need == 0 || be <= avail);
         tok[lane + 1] = te;
         blk[lane + 1] = be;
@@ -111,67 +111,71 @@ __global__ __launch_bounds__(NT) void cache_plan_kernel(CachePlanParams p)
             tok[0] = t;
             blk[0] = b;
         }
-        held[lane] = (int32_t)q.cached;
+        held[lane] = q.cached;
         granted[lane] = ok;
         if (blockIdx.y == 0) {
             if (lane < n) {
-                p.cu[first + lane] = (int32_t)min(te - q.fresh, (int64_t)INT32_MAX);
-                p.seqlens[first + lane] = (int32_t)(ok ? q.cached + q.fresh : q.cached);
+                p.cu[first + lane] = te - q.fresh;
+                p.seqlens[first + lane] = ok ? q.cached + q.fresh : q.cached;
             }
             if (last_x) {
-                const int64_t te_all = __shfl(te, 63), need_all = __shfl(be, 63);
-                int64_t taken = need_all;
-                if (need_all > avail) {
+                int32_t taken = last_lane(be);
+                if (taken > avail) {
                     // more asked for than there is: the largest prefix sum of need that
                     // some granted request reaches
                     taken = 0;
-                    int64_t sofar = 0;
+                    int32_t sofar = 0;
                     for (int r0 = 0; r0 < p.batch && sofar <= avail; r0 += 64) {
-                        const int64_t need = r0 + lane < p.batch ? request(p, r0 + lane).need : 0;
-                        const int64_t e = sofar + wave_scan(need, lane);
-                        int64_t best = e <= avail ? e : 0;
+                        const int32_t need = r0 + lane < p.batch ? request(p, r0 + lane).need : 0;
+                        const int32_t e = sofar + wave_scan(need);
+                        int32_t best = e <= avail ? e : 0;
 #pragma unroll
                         for (int d = 1; d < 64; d <<= 1) best = max(best, __shfl_xor(best, d));
                         taken = max(taken, best);
-                        sofar = __shfl(e, 63);
+                        sofar = last_lane(e);
                     }
                 }
                 if (lane == 0) {
-                    p.cu[p.batch] = (int32_t)min(te_all, (int64_t)INT32_MAX);
-                    *p.num_free_out = (int32_t)(avail - taken);
+                    p.cu[p.batch] = last_lane(te);
+                    *p.num_free_out = avail - taken;
                 }
             }
         }
     }
     __syncthreads();
     if (n > 0) {
+        const int32_t b1 = (1 << p.bshift) - 1;
         const int64_t step = (int64_t)gridDim.y * NT, at = (int64_t)blockIdx.y * NT + tid;
-        const int64_t b1 = (1 << p.bshift) - 1;
-        // new blocks (a refused request's lie past the free list's end)
-        const int64_t bend = min(blk[n], avail);
-        for (int64_t i = blk[0] + at; i < bend; i += step) {
-            const int r = find(blk, n, i);
-            if (!granted[r]) continue;
-            const int64_t col = ((held[r] + b1) >> p.bshift) + (i - blk[r]);
-            p.table[(first + r) * p.stride_table + col] = p.free_blocks[avail - 1 - i];
-        }
         // new tokens
-        const int64_t tend = min(tok[n], p.total_new);
-        for (int64_t i = tok[0] + at; i < tend; i += step) {
-            const int r = find(tok, n, i);
+        const int64_t tend = min((int64_t)tok[n], p.total_new);
+        for (int64_t i = max(tok[0], 0) + at; i < tend; i += step) {
+            const int r = find(tok, n, (int32_t)i);
             int64_t slot = -1;
             if (granted[r]) {
-                const int64_t pos = held[r] + (i - tok[r]);
-                const int64_t col = pos >> p.bshift, from = (held[r] + b1) >> p.bshift;
-                const int32_t block = col < from ? p.table[(first + r) * p.stride_table + col]
-                                                 : p.free_blocks[avail - 1 - (blk[r] + col - from)];
+                const int32_t pos = held[r] + ((int32_t)i - tok[r]);
+                const int32_t col = pos >> p.bshift, from = (held[r] + b1) >> p.bshift;
+                const int32_t up = avail - 1 - (blk[r] + col - from);
+                int32_t block = -1;
+                if (col < from) {
+                    if (col >= 0 && col < p.width) block = p.table[(first + r) * p.stride_table + col];
+                } else if (up >= 0 && up < p.free_len) {
+                    block = p.free_blocks[up];
+                }
                 if (block >= 0) slot = ((int64_t)block << p.bshift) + (pos & b1);
             }
             p.slots[i] = slot;
         }
+        // new blocks (a refused request's lie past the free list's end)
+        const int64_t bend = min(blk[n], avail);
+        for (int64_t i = max(blk[0], 0) + at; i < bend; i += step) {
+            const int r = find(blk, n, (int32_t)i);
+            const int32_t col = ((held[r] + b1) >> p.bshift) + ((int32_t)i - blk[r]);
+            if (granted[r] && col >= 0 && col < p.width)
+                p.table[(first + r) * p.stride_table + col] = p.free_blocks[avail - 1 - i];
+        }
     }
     if (last_x) {
-        const int64_t end = n > 0 ? tok[n] : 0;
+        const int64_t end = n > 0 ? max(tok[n], 0) : 0;
         for (int64_t i = end + (int64_t)blockIdx.y * NT + tid; i < p.total_new;
              i += (int64_t)gridDim.y * NT)
             p.slots[i] = -1;
@@ -183,8 +187,8 @@ __global__ __launch_bounds__(NT) void cache_plan_kernel(CachePlanParams p)
 hipError_t launch_cache_plan(const CachePlanParams& p, hipStream_t stream)
 {
     const int64_t x = p.batch > 0 ? ((int64_t)p.batch + kReqs - 1) / kReqs : 1;
-    // about 1024 tokens for each workgroup of one group of requests
-    int64_t y = p.total_new / (x * 1024) + 1;
+    // about a token for each thread
+    int64_t y = p.total_new / (x * NT) + 1;
     if (y > 256) y = 256;
     hipLaunchKernelGGL(cache_plan_kernel, dim3((unsigned)x, (unsigned)y), dim3(NT), 0, stream, p);
     return hipGetLastError();
