@@ -1,5 +1,6 @@
 /*
- * attn.h -- C ABI of the gfx950 fused attention forward library (libattn.so).
+ * attn.h -- C ABI of the gfx950 fused attention forward library (libattn.so):
+ * attention over tensors (attn_fwd) and over an 8-bit block cache (attn_cache_*).
  *
  * The library computes the forward pass of scaled-dot-product attention,
  * O = Norm(Mask(Score(scale * Q K^T))) V (Eq. 1 of Section 2.2 and the
@@ -393,7 +394,8 @@ int attn_cache_append(const void *k, const void *v, const attn_cache *cache,
  * reach others of the same request. Packed rows behind the last request's keep
  * their output. Arithmetic: products of the stored values with q in bf16 matrix
  * instructions and fp32 sums, the scales applied in fp32 (fp32 q and P are split
- * into three bf16 terms, so nothing is lost).
+ * into three bf16 terms, so nothing is lost). q . x is summed before the scale of
+ * the stored x: |q| up to 2^104 keeps it in range.
  * The workspace is that of attn_fwd_ws: attn_cache_workspace_bytes says how much
  * the call can use (a quarter of the bytes of q, out, K and V at most, or 256 MiB
  * where that is more), NULL or less computes it without splitting the keys.

@@ -151,7 +151,7 @@ extern "C" const char* attn_status_string(int status)
     case ATTN_ERR_BAD_VARIANT: return "bad mask or norm kind, window, scale, soft-cap, prefix or segments";
     case ATTN_ERR_ALIGNMENT: return "pointer or stride not 16-byte aligned";
     case ATTN_ERR_UNSUPPORTED: return "head_dim, dtype or size outside the compiled set";
-    case ATTN_ERR_ABI: return "attn_variant_desc.struct_size does not match the library";
+    case ATTN_ERR_ABI: return "a descriptor's struct_size does not match the library";
     case ATTN_ERR_LAUNCH: return "the HIP kernel launch failed";
     default: return "unknown status";
     }

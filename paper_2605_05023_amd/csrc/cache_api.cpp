@@ -248,8 +248,8 @@ int check_fwd(const attn_cache* cache, const attn_cache_fwd_desc& d, CacheFwdPar
     if (d.max_seqlen_k < 0 || d.table_width < 0 || d.stride_table < 0) return ATTN_ERR_BAD_SHAPE;
     p.stride_table = d.stride_table ? d.stride_table : d.table_width;
     if (d.batch > 1 && p.stride_table < d.table_width) return ATTN_ERR_BAD_SHAPE;
-    // keys are numbered with 31 bits, a chunk past the last included
-    if ((int64_t)d.table_width << p.pool.bshift > kInt32Max - 2 * kChunkKeys) return ATTN_ERR_UNSUPPORTED;
+    // keys are numbered with 31 bits, those of the chunks looked at ahead included
+    if ((int64_t)d.table_width << p.pool.bshift > kInt32Max - 32 * kChunkKeys) return ATTN_ERR_UNSUPPORTED;
     const int64_t max_q = packed ? std::min<int64_t>(d.max_seqlen_q, d.total_q) : d.seqlen_q;
     const int64_t D = cache->head_dim, align = d.dtype == ATTN_BF16 ? 8 : 4;
     const int64_t rows = packed ? 0 : max_q;
@@ -407,6 +407,12 @@ void plan_schedule(const attn_cache_fwd_desc& d, FwdShape& s, CacheFwdParams& p,
                 p.row_tiles = (int32_t)row_tiles;
                 p.splits = (int32_t)splits;
                 p.split_chunks = splits > 1 ? (int32_t)per : 1 << 30;
+                // More workgroups than fit at once, whole requests each: the longest first
+                // (packed prompts 254 -> 211 and 697 -> 516 us, decode of 64 requests of up
+                // to 16000 keys 233 -> 198; with the keys split, or four wavefronts of few
+                // rows, finding the order costs as much as it gives).
+                p.by_length = splits == 1 && items > slots && p.batch > 1 && p.batch <= 64 &&
+                              (c.many || c.waves == 8);
             }
             if (d.sched_splits) break;
         }

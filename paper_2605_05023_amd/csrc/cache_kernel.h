@@ -92,10 +92,23 @@ __device__ __forceinline__ int split_size(const CacheFwdParams& p, int chunks)
     return max(p.split_chunks, (chunks + p.splits - 1) / p.splits);
 }
 
+// The request of rank n by its number of keys, longest first (batch <= 64).
+__device__ __forceinline__ uint32_t nth_longest(const CacheFwdParams& p, uint32_t n)
+{
+    const int lane = threadIdx.x & 63, mine = lane < p.batch ? max(p.seqlens[lane], 0) : -1;
+    uint32_t rank = 0;
+    for (int j = 0; j < p.batch; ++j) {
+        const int other = __builtin_amdgcn_readlane(mine, j);
+        rank += other > mine || (other == mine && j < lane);
+    }
+    return (uint32_t)__builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == n && lane < p.batch));
+}
+
 // Work item -> (kv group, row tile): the row tiles of a group follow one another
 // and, when the groups are a multiple of eight, on one XCD (ids are dealt
 // round-robin over the 8 XCDs), so that they meet in its L2. The last ones, which
-// see the most keys under a causal mask, come first.
+// see the most keys under a causal mask, come first, and (by_length) the requests
+// with the most keys: the workgroups that are left at the end are short ones.
 __device__ __forceinline__ void work_item(const CacheFwdParams& p, uint32_t id, uint32_t* g, uint32_t* rt)
 {
     const uint32_t groups = (uint32_t)(p.batch * p.pool.hkv), nrt = (uint32_t)p.row_tiles;
@@ -108,6 +121,10 @@ __device__ __forceinline__ void work_item(const CacheFwdParams& p, uint32_t id, 
         *g = id / nrt;
     }
     *rt = nrt - 1 - *rt;
+    if (p.by_length) {
+        const uint32_t n = fast_div(*g, p.div_hkv), h = *g - n * (uint32_t)p.pool.hkv;
+        *g = nth_longest(p, n) * (uint32_t)p.pool.hkv + h;
+    }
 }
 
 template <bool E5M2, bool HI>

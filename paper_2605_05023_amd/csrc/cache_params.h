@@ -67,6 +67,7 @@ struct CacheFwdParams {
     // Flat row f of a kv group is query f / group of head f % group;
     // row_tiles tiles of tile_rows flat rows for each kv group.
     int32_t row_tiles, tile_rows;
+    int32_t by_length;       // longest requests first (at most 64 of them)
     // Key splits: `splits` workgroups share a row tile's chunks of 64 keys, at
     // least split_chunks each. Partials, in the order of the LSE's ws_rows rows:
     // ws_o [splits][ws_rows][D], ws_ml the same with (running max, row sum).

@@ -318,9 +318,9 @@ def schedules(c):
     yield dict(kernel=2, waves=4 if d == 64 else 8, splits=2)
 
 
-def check_case(c, **how):
+def check_case(c, scheds=None, **how):
     got = []
-    for sched in [None] if "lib" in how else schedules(c):
+    for sched in scheds or ([None] if "lib" in how else schedules(c)):
         out, lse = run_case(c, schedule=sched, **how)
         assert bool(torch.isfinite(out.float()).all()), sched
         got.append((sched, out, lse))
@@ -395,6 +395,18 @@ def test_longer_than_told():
     c = attention_case(lens=[(1, 9001), (1, 100)], seed=12)
     check_case(c, max_k=3000)
     check_case(c, max_k=0)
+
+
+@pytest.mark.parametrize("batch", [40, 64, 65])
+def test_longest_first(batch):
+    """More workgroups than fit the chip at once, whole requests each (up to 64 of them in the
+    order of their lengths): equal lengths, none, one token, and many."""
+    rng = random.Random(batch)
+    lens = [(1, rng.choice([0, 1, 5, 5, 70, rng.randint(1, 400)])) for _ in range(batch)]
+    few = attention_case(d=64, hq=8, hkv=8, bs=16, lens=lens, seed=60)
+    many = attention_case(d=64, hq=32, hkv=8, bs=16, lens=[(rng.choice([0, 1, 33]), lk) for _, lk in lens], seed=61)
+    check_case(few, [dict(kernel=1, waves=8, tiles=1, splits=1), dict(kernel=1, waves=4, tiles=1, splits=1)])
+    check_case(many, [dict(kernel=2, waves=4, splits=1)])
 
 
 @pytest.mark.parametrize("n", [1, 40])
@@ -494,6 +506,38 @@ def test_nan_reaches_the_rows_that_see_it():
         out, lse = run_case(c, schedule=sched)
         assert torch.isnan(out[0, 0].float()).all() and torch.isnan(lse[0, 0])
         assert torch.isfinite(out[0, 1].float()).all() and torch.isfinite(lse[0, 1])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_large_queries(dt):
+    """Queries of 2^104, the largest whose products with any stored values stay finite, against
+    keys small enough to keep the scores in range."""
+    c = attention_case(dt=dt, d=128, hq=2, hkv=1, lens=[(2, 90)], seed=62)
+    c["pool"][2].mul_(2.0 ** -104)
+    c["q"] = c["q"].clamp(-1, 1) * 2.0 ** 104
+    check_case(c)
+
+
+def test_captured_split_call():
+    """A split call and its workspace in two graphs, replayed in turn with new queries."""
+    c = attention_case(lens=[(1, 9001), (1, 3000)], seed=63)
+    cache = attn.KVCache(*(t.to(DEV) for t in c["pool"]))
+    q, table, lens, cu = c["q"].to(DEV), c["table"].to(DEV), i32([9001, 3000]), i32([0, 1, 2])
+    kw = dict(causal=True, cu_seqlens_q=cu, max_seqlen_q=1)
+    attn.cache_fwd(q, cache, table, lens, **kw)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(attn.cache_fwd(q, cache, table, lens, **kw))
+        graphs.append(g)
+    for step in range(4):
+        q.copy_(torch.randn(q.shape, generator=gen(step)))
+        want = attn.cache_fwd(q, cache, table, lens, **kw)
+        for g, (o, l) in zip(graphs, outs):
+            g.replay()
+            assert bytes_equal(o, want[0]) and torch.equal(l, want[1])
 
 
 def test_far_pages():
