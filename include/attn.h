@@ -395,7 +395,8 @@ int attn_cache_append(const void *k, const void *v, const attn_cache *cache,
  * their output. Arithmetic: products of the stored values with q in bf16 matrix
  * instructions and fp32 sums, the scales applied in fp32 (fp32 q and P are split
  * into three bf16 terms, so nothing is lost). q . x is summed before the scale of
- * the stored x: |q| up to 2^104 keeps it in range.
+ * the stored x, and P is up to 2^8: |q| up to 2^104 and |v| up to 2^96 keep it in
+ * range. Shares of V below about 2^-110 may be lost.
  * The workspace is that of attn_fwd_ws: attn_cache_workspace_bytes says how much
  * the call can use (a quarter of the bytes of q, out, K and V at most, or 256 MiB
  * where that is more), NULL or less computes it without splitting the keys.

@@ -219,23 +219,25 @@ enum : int { kModsNone = 0, kModsAlibi = 1, kModsCapShort = 2, kModsCapExact = 3
 // What the softmax of one 16-row tile needs of the chunk: scores s of this lane's
 // sixteen keys (from `key` on) under the scales ks and vs of their block.
 struct ChunkScales {
-    float ks, lvs, ivs;  // K's scale; log2 and inverse of V's (of 1 where that is 0)
-    bool no_v;           // V's scale is 0
+    float ks, vs;        // 0 without a block
+    float lvs, ivs;      // log2 and inverse of vs (of 1 where it is tiny)
+    bool tiny;           // vs is 0, or so small that P vs would leave the normal numbers
     int key, page;       // first key; its block, -1: none
-    bool whole;          // every row of the wavefront sees all 64 keys, and no vs is 0
+    bool whole;          // every row of the wavefront sees all 64 keys, and no vs is tiny
 };
 
 __device__ __forceinline__ ChunkScales chunk_scales(float ks, float vs, int key, int page, bool inside)
 {
     ChunkScales c;  // (a page that is not there: scales of 0 in place of block 0's)
-    c.no_v = page < 0 || !(vs > 0.0f);
-    const float v = c.no_v ? 1.0f : vs;
     c.ks = page < 0 ? 0.0f : ks;
+    c.vs = page < 0 ? 0.0f : vs;
+    c.tiny = !(c.vs >= 0x1p-80f);
+    const float v = c.tiny ? 1.0f : vs;
     c.lvs = __builtin_amdgcn_logf(v);
     c.ivs = __builtin_amdgcn_rcpf(v);
     c.key = key;
     c.page = page;
-    c.whole = inside && __builtin_amdgcn_ballot_w64(c.no_v) == 0;
+    c.whole = inside && __builtin_amdgcn_ballot_w64(c.tiny) == 0;
     return c;
 }
 
@@ -311,17 +313,24 @@ __device__ __forceinline__ void softmax_exp(const f32x4 (&s)[4], const ChunkScal
     sum = __builtin_fmaf((add[0] + add[1]) + (add[2] + add[3]), c.ivs, sum);
 }
 
-// Where V's scale is 0: no share of V, whatever its bytes.
+// Where V's scale is tiny (that of a block of zeros is 2^-120), softmax_exp left it
+// out, so that the row sum has all of P, and it comes in here. P vs below fp32's
+// normal numbers may be lost.
 template <int MT, int NS>
-__device__ __forceinline__ void drop_v(const ChunkScales& c, bf16x8 (&pf)[MT][2][NS])
+__device__ __forceinline__ void scale_tiny(const ChunkScales& c, bf16x8 (&pf)[MT][2][NS])
 {
-    if (!c.whole && c.no_v) {
+    if (!c.whole && c.tiny) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int n = 0; n < NS; ++n) pf[m][k][n] = bf16x8{};
+                for (int e = 0; e < 8; ++e) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int n = NS - 1; n >= 0; --n) x += (float)pf[m][k][n][e];
+                    split_p<NS>(x * c.vs, pf[m][k], e);
+                }
     }
 }
 
@@ -529,7 +538,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_fwd_kernel(CacheFwdParams
                 softmax_max<DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m]);
             softmax_exp<NS>(s[m], cs, factor, mx[m], sum[m], pf[m]);
         }
-        drop_v<MT, NS>(cs, pf);
+        scale_tiny<MT, NS>(cs, pf);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll

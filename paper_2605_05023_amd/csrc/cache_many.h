@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache_many_kernel(CacheFwdParam
                     softmax_max<DT, MODS>(p, s[m], cs, jlo[m], jhi[m], ip[m], slope[m], mx[m], sum[m], acc[m]);
                 softmax_exp<NS>(s[m], cs, factor, mx[m], sum[m], pf[m]);
             }
-            drop_v<MT, NS>(cs, pf);
+            scale_tiny<MT, NS>(cs, pf);
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
