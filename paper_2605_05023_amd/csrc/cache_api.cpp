@@ -307,22 +307,23 @@ int64_t workspace_need(const CacheFwdParams& p, int64_t D)
 
 // The schedules of a call: kernel, wavefronts of a workgroup, 16-row tiles of a
 // wavefront; microseconds that a launch, a round of one chunk for each wavefront
-// (many rows: for the workgroup) and a chunk's products and softmax on one SIMD
-// take, head dim 128 and bf16; workgroups that fit the chip at once (bf16 of
-// D = 128, of D = 64, fp32 likewise). Fitted to 348 calls of every kind (1..4096
-// queries, 1..128 requests, 200..32000 keys, D = 64 and 128, bf16 and fp32) that
+// (many rows: for the workgroup), a chunk's products and softmax on one SIMD, and
+// the start of a row tile that another workgroup does not cover take, head dim 128
+// and bf16; workgroups that fit the chip at once (bf16 of D = 128, of D = 64, fp32
+// likewise). Fitted to 460 calls of every kind (1..4096 queries, 1..128 requests of
+// equal and of uneven lengths, 200..32000 keys, D = 64 and 128, bf16 and fp32) that
 // were timed under each schedule and up to 64 splits: what plan_schedule takes is
-// 1.1 % over the fastest on average, 4 % at the 90th percentile, 21 % at most.
+// 1.6 % over the fastest on average, 7 % at the 90th percentile, 22 % at most.
 struct Schedule {
     bool many;
     int waves, tiles;
-    double launch, round, tile;
+    double launch, round, tile, start;
     int slots128, slots64, slots128f, slots64f;
 };
 constexpr Schedule kSchedules[] = {
-    {false, 4, 1, 4.3, 1.55, 1.15, 768, 1280, 512, 768}, {false, 8, 1, 4.4, 1.95, 1.15, 256, 512, 256, 256},
-    {false, 4, 2, 5.4, 2.3, 1.5, 512, 768, 0, 0},        {false, 8, 2, 4.9, 2.6, 1.5, 256, 256, 0, 0},
-    {true, 4, 2, 4.6, 1.6, 1.6, 512, 768, 512, 768},     {true, 8, 2, 3.8, 1.85, 0.95, 256, 0, 256, 0},
+    {false, 4, 1, 3.75, 1.68, 1.04, 0.0, 768, 1280, 512, 768}, {false, 8, 1, 4.11, 1.77, 1.04, 0.0, 256, 512, 256, 256},
+    {false, 4, 2, 7.04, 2.0, 0.82, 0.0, 512, 768, 0, 0},       {false, 8, 2, 5.11, 2.49, 0.82, 0.0, 256, 256, 0, 0},
+    {true, 4, 2, 5.12, 1.56, 1.01, 0.9, 512, 768, 512, 768},   {true, 8, 2, 3.51, 1.61, 0.8, 2.24, 256, 0, 256, 0},
 };
 
 // Choose kernel, tile and key splits by the time that the model above expects: of
@@ -343,14 +344,14 @@ void plan_schedule(const attn_cache_fwd_desc& d, FwdShape& s, CacheFwdParams& p,
     const int64_t limit = std::max<int64_t>(bytes / 4, (int64_t)256 << 20);
     p.ws_rows = rows * p.hq;
     const int64_t part = p.ws_rows * (D + 2) * (int64_t)sizeof(float);
-    const bool d64 = D == 64, f32 = s.kind.fp32;
+    const bool d64 = D == 64, f32 = s.kind.fp32, ragged = d.cu_seqlens_q && d.batch > 1;
     double best = 1e30;
     for (const Schedule& c : kSchedules) {
         const int tiles = f32 ? 1 : c.tiles;
         const int slots = f32 ? d64 ? c.slots64f : c.slots128f : d64 ? c.slots64 : c.slots128;
         if (slots == 0) continue;
-        const double round = c.round * (d64 ? 0.67 : 1.0) * (!f32 ? 1.0 : c.many ? 1.0 : 1.36);
-        const double tile = c.tile * (d64 ? 0.5 : 1.0) * (!f32 ? 1.0 : c.many ? 1.0 : 1.55);
+        const double round = c.round * (d64 ? 0.66 : 1.0) * (!f32 ? 1.0 : c.many ? 1.35 : 1.47);
+        const double tile = c.tile * (d64 ? 0.58 : 1.0) * (!f32 ? 1.0 : c.many ? 1.35 : 1.72);
         const bool forced = d.sched_kernel || d.sched_waves || d.sched_tiles;
         if (forced) {
             if ((d.sched_kernel && c.many != (d.sched_kernel == 2)) ||
@@ -384,15 +385,22 @@ void plan_schedule(const attn_cache_fwd_desc& d, FwdShape& s, CacheFwdParams& p,
             for (const double fill : {1.0, 0.6}) {
                 const double avg = std::max(1.0, fill * seen), share = splits > 1 ? 1.0 : avg / (double)chunks;
                 const double parts = std::max(1.0, used * fill), turns = items * parts / slots;
-                const double chain = rounds * (turns > 1 ? std::max(1.0, turns * share + 0.6) : 1.0);
+                // (the turns of a split call are of one length, and the last may be part full)
+                const double queue = turns <= 1 ? 1.0
+                                     : splits == 1
+                                         ? std::max(1.0, turns * share + (ragged ? 0.39 : 0.5))
+                                         : ragged ? turns + 0.57
+                                                  : 0.23 * std::ceil(turns) + 0.77 * (turns + 0.5);
+                const double chain = rounds * queue + c.start * (d64 ? 0.66 : 1.0) * std::max(1.0, turns);
                 const double work = items * avg * (c.many ? c.waves : 1) / 1024 * tile;
-                const double memory = (double)heads * avg * (double)(kChunkKeys * 2 * D) / 8.7e6;
+                const double memory = (double)heads * avg * (double)(kChunkKeys * 2 * D) / 9.45e6;
                 const double most = std::max({chain, work, memory});
-                double one = c.launch + 0.0033 * items * parts * (c.waves / 4) + most +
-                             0.2 * (chain + work + memory - most);
+                double one = c.launch + 0.0035 * items * parts * (c.waves / 4) + most +
+                             0.22 * (chain + work + memory - most);
                 if (splits > 1)  // the second launch, the partial rows, and the host's time for two
-                    one = std::max(one + 2.7 + 2 * parts * (double)part / 3.6e6, 10.0);
-                us += std::max(one, 6.4);
+                    one = std::max(one + 2.48 + 2 * parts * (double)part / 4.18e6, 10.0);
+                // (uneven lengths: more is left over at the end of wide workgroups)
+                us += std::max(one, 6.4) * (ragged && c.many && c.waves == 8 ? 1.12 : 1.0);
                 if (p.batch == 1) {
                     us *= 2;
                     break;
