@@ -4,7 +4,8 @@
 // LSE = (m + log2 sum w_s l_s) ln 2. One wavefront per row: 16-byte pieces of
 // O, D / 4 lanes side by side, the splits 256 / D apart. It finds the splits of
 // its row tile as the attention kernel did; a tile that was not split is
-// written already. Bound by the latency of its loads.
+// written already. Bound by the latency of its loads, or memory where the
+// partials are many (106 MB 33 us).
 #include "cache_kernel.h"
 
 namespace attn {
